@@ -101,9 +101,10 @@ def draw(rng):
         c["layers"], c["tokens"] = _log_int(rng, 1, 32), rng.choice((1, _log_int(rng, 2, 5000)))
         c["ctx"] = c["tokens"] + _log_int(rng, 1, 3000)
     elif op == "select":
-        c["ctx"] = _log_int(rng, 200, 400000)
         c["first"], c["last"] = rng.randrange(0, 5), rng.randrange(1, 9)
-        c["sel"] = c["first"] + c["last"] + _log_int(rng, 1, 300)
+        always = c["first"] + c["last"]
+        c["ctx"] = max(_log_int(rng, 200, 400000), (always + 8) * c["block"])
+        c["sel"] = always + _log_int(rng, 1, min(300, (c["ctx"] // c["block"] - always) // 2))
     elif op == "blocks":
         c["ctx"], c["sel"] = _log_int(rng, 40, 60000), _log_int(rng, 1, 256)
     else:
@@ -116,7 +117,8 @@ def draw(rng):
     while w["bytes"] > 250e6 or w["flops"] > 400e9 or _rows(c) > 2.5e6 or _scores(c) > 1.0e9:
         k = rng.choice([k for k in ("batch", "layers", "ctx", "tokens", "heads") if c[k] > 1])
         if k == "ctx":
-            c["ctx"] = max(c["tokens"], c["ctx"] * 2 // 3)
+            c["ctx"] = max(c["tokens"], (c["sel"] + 2) * c["block"] if op == "select" else 1,
+                           c["ctx"] * 2 // 3)
         else:
             c[k] = max(1, c[k] * 2 // 3)
         w = work(c)
