@@ -35,7 +35,7 @@
 extern "C" {
 #endif
 
-#define TVQ_ABI_VERSION 3
+#define TVQ_ABI_VERSION 4
 #define TVQ_MAX_LAYERS 256
 
 typedef enum {
@@ -277,6 +277,103 @@ tvq_status tvq_attention_paged(const tvq_codec* c, const void* pool, const tvq_l
                                int32_t layer, int32_t num_q_heads, float scale, tvq_dtype q_dtype,
                                const void* q, tvq_dtype o_dtype, void* o, void* workspace,
                                int64_t workspace_bytes, void* stream);
+
+/* ---- many new tokens (prompts, draft tokens) ----
+ * Causal attention of the newest in->tokens tokens of every sequence over one layer of the cache,
+ * from the codes.  Token j of a sequence's n new ones stands at position ctx - n + j and attends to
+ * the positions 0 .. ctx - n + j, its own included (so its K and V are encoded first); a position
+ * below 0 attends to nothing and gives zeros.  Scores, weights and the decoded vectors are those of
+ * tvq_attention_decode.
+ *   q, o       device views [B][num_q_heads][T][d] described by q_desc and o_desc (batch B, tokens
+ *              T, strides in elements, stride_l ignored), bf16 or fp32; every vector starts on a
+ *              16-byte boundary, and the vectors of o lie apart
+ *   t_end      contiguous cache: the context of every sequence, T .. lay->capacity_tokens
+ *   ctx_lens   paged: device int32 [B], clipped to max_ctx (host, 1 .. max_blocks * block_tokens);
+ *              <= 0 gives zeros.  The positions below them must lie in blocks the table holds
+ *   q_lens     paged: device int32 [B], new tokens per sequence, clipped to 0 .. T; rows behind them
+ *              are not written.  NULL: T for all
+ *   workspace  device scratch of at least tvq_attention_prefill_workspace(...) bytes, 16-byte
+ *              aligned; NULL where that is 0
+ * The products run on the fp16 matrix cores with fp32 accumulation, operands scaled by powers of
+ * two into fp16's range.  bf16 o: queries, rebuilt pairs and softmax weights are rounded to fp16
+ * (11 bits) once each.  fp32 o: each is a pair of fp16 numbers (22 bits; expect ~1e-6 relative to
+ * an fp64 evaluation).
+ * Supported: d = 64 or 128, at most 64 query heads per KV head, n = 64, 128 or 256 with 8-bit linear
+ * or 4-bit log-space norms for both K and V of the layer (TVQ_ERR_UNSUPPORTED otherwise).  Launches
+ * one kernel on `stream`, two where the workspace is not empty; T == 0 launches nothing. */
+tvq_status tvq_attention_prefill_workspace(const tvq_codec* c, int64_t batch, int32_t num_q_heads,
+                                           int64_t tokens, int64_t max_ctx, int64_t* bytes);
+tvq_status tvq_attention_prefill(const tvq_codec* c, const void* cache, const tvq_layout* lay,
+                                 int32_t layer, int64_t t_end, int32_t num_q_heads, float scale,
+                                 tvq_dtype q_dtype, const void* q, const tvq_tensor_desc* q_desc,
+                                 tvq_dtype o_dtype, void* o, const tvq_tensor_desc* o_desc,
+                                 void* workspace, int64_t workspace_bytes, void* stream);
+tvq_status tvq_attention_prefill_paged(const tvq_codec* c, const void* pool,
+                                       const tvq_layout* pool_layout, const int32_t* block_table,
+                                       int32_t max_blocks, const int32_t* ctx_lens,
+                                       int64_t max_ctx, const int32_t* q_lens, int32_t layer,
+                                       int32_t num_q_heads, float scale, tvq_dtype q_dtype,
+                                       const void* q, const tvq_tensor_desc* q_desc,
+                                       tvq_dtype o_dtype, void* o, const tvq_tensor_desc* o_desc,
+                                       void* workspace, int64_t workspace_bytes, void* stream);
+
+/* ---- part of a long context ----
+ * Bounds of the keys of every pool block: for layer l, pool block j and KV head h the smallest and
+ * the largest value of each channel over the keys written to it, bf16 [L][n_blocks][H][2][d] (lo,
+ * hi) in device memory of tvq_key_bounds_bytes(...) bytes that the caller owns, 16-byte aligned.
+ * fp32 keys are rounded outward, values beyond the largest finite bf16 to it; a NaN is passed over
+ * (a channel without a number has lo > hi).  They are bounds of the keys as given, not of the
+ * decoded ones. */
+tvq_status tvq_key_bounds_bytes(const tvq_codec* c, const tvq_layout* pool_layout, int64_t* bytes);
+
+/* Update the bounds with the keys of a tvq_encode_paged call: the same in_dtype, k, in, positions
+ * and block table, and the same rule of what is written.  A block whose row 0 the call writes starts
+ * anew; the others are merged with what they hold, so blocks must be filled from row 0 on.  Two
+ * sequences of one call must not write to the same block.  One kernel launch. */
+tvq_status tvq_key_bounds_paged(const tvq_codec* c, tvq_dtype in_dtype, const void* k,
+                                const tvq_tensor_desc* in, const int32_t* positions,
+                                const int32_t* block_table, int32_t max_blocks, void* bounds,
+                                const tvq_layout* pool_layout, void* stream);
+
+/* For one new token per sequence and each KV head, the n_sel blocks of the sequence's context that
+ * score highest, score(i) = max over the head's query heads of
+ *   sum_c max(q_c, 0) hi_ic + min(q_c, 0) lo_ic,
+ * an upper bound of q . k over the keys of block i; the sum in fp64, rounded to fp32.  A query head
+ * with an element that is not finite scores lowest, ties go to the lower block.  The first n_first blocks and the last n_last are
+ * always among them (n_first >= 0, n_last >= 1, n_first + n_last <= n_sel).
+ *   q          device [B][num_q_heads][d], contiguous, bf16 or fp32, 16-byte aligned
+ *   ctx_lens   device int32 [B], clipped to max_ctx (1 .. max_blocks * block_tokens)
+ *   blocks     device int32 [B][H][n_sel]: block numbers of the sequence (its table's entries) in
+ *              ascending order, -1 behind them
+ *   sel_lens   device int32 [B][H]: the tokens of the context in these blocks
+ *   workspace  tvq_select_blocks_workspace(...) bytes, 16-byte aligned
+ * A table entry that holds no pool block is read as block 0.  n_sel <= 65536, and at most 64 query
+ * heads per KV head.  Two kernel launches. */
+tvq_status tvq_select_blocks_workspace(const tvq_codec* c, int64_t batch, int64_t max_ctx,
+                                       int64_t block_tokens, int64_t* bytes);
+tvq_status tvq_select_blocks(const tvq_codec* c, const void* bounds, const tvq_layout* pool_layout,
+                             const int32_t* block_table, int32_t max_blocks,
+                             const int32_t* ctx_lens, int64_t max_ctx, int64_t batch,
+                             int32_t layer, int32_t num_q_heads, tvq_dtype q_dtype, const void* q,
+                             int32_t n_sel, int32_t n_first, int32_t n_last, int32_t* blocks,
+                             int32_t* sel_lens, void* workspace, int64_t workspace_bytes,
+                             void* stream);
+
+/* Attention of one query token per sequence (as tvq_attention_paged) over listed blocks: KV head h of
+ * sequence b attends to the first sel_lens[b][h] slots of blocks[b][h][0], blocks[b][h][1], ... in
+ * this order, block_tokens slots each (so only the last block that a list uses can be partly
+ * filled); <= 0 gives a zero output, more than n_sel * block_tokens is clipped.  Entries are block
+ * numbers of the sequence; one outside its table, or whose table entry holds no pool block, is read
+ * as pool block 0 (memory-safe, meaningless values).  A block listed twice counts twice.
+ * Arithmetic, formats and launches are those of tvq_attention_prefill.  n_sel * block_tokens < 2^31. */
+tvq_status tvq_attention_blocks_workspace(const tvq_codec* c, int64_t batch, int32_t num_q_heads,
+                                          int64_t n_sel, int64_t block_tokens, int64_t* bytes);
+tvq_status tvq_attention_blocks(const tvq_codec* c, const void* pool, const tvq_layout* pool_layout,
+                                const int32_t* block_table, int32_t max_blocks,
+                                const int32_t* blocks, int32_t n_sel, const int32_t* sel_lens,
+                                int64_t batch, int32_t layer, int32_t num_q_heads, float scale,
+                                tvq_dtype q_dtype, const void* q, tvq_dtype o_dtype, void* o,
+                                void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Bits per element of the codec, averaged over layers and over K and V.
  * accounting 0: the paper's -- eq. (1) angle bits (log2 n)/2 (fractional for non-power-of-

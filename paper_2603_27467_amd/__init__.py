@@ -18,6 +18,9 @@ from ._capi import (  # noqa: F401
     tvq_attention_decode, tvq_attention_decode_noalloc, TVQ_ERR_SCRATCH,
     TVQ_ATTENTION_SCRATCH_BYTES,
     tvq_encode_mfma, tvq_encode_paged, tvq_decode_paged, tvq_attention_paged_workspace, tvq_attention_paged,
+    tvq_attention_prefill_workspace, tvq_attention_prefill, tvq_attention_prefill_paged,
+    tvq_key_bounds_bytes, tvq_key_bounds_paged, tvq_select_blocks_workspace, tvq_select_blocks,
+    tvq_attention_blocks_workspace, tvq_attention_blocks,
     tvq_abi_version, library_path, load_library,
 )
 from .codec import Codec, LayerCfg, desc_of  # noqa: F401

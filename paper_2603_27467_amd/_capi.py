@@ -6,7 +6,7 @@ import os
 
 import numpy as np
 
-TVQ_ABI_VERSION = 3
+TVQ_ABI_VERSION = 4
 TVQ_MAX_LAYERS = 256
 TVQ_OK, TVQ_ERR_INVALID_ARG, TVQ_ERR_UNSUPPORTED, TVQ_ERR_HIP, TVQ_ERR_ALLOC = 0, -1, -2, -3, -4
 TVQ_ERR_SCRATCH = -5
@@ -103,6 +103,25 @@ def load_library():
     L.tvq_attention_paged.argtypes = [vp, vp, ctypes.POINTER(tvq_layout), vp, i32, vp, i64, i64,
                                       i32, i32, ctypes.c_float, ctypes.c_int, vp, ctypes.c_int,
                                       vp, vp, i64, vp]
+    desc, lay = ctypes.POINTER(tvq_tensor_desc), ctypes.POINTER(tvq_layout)
+    for name, args in {
+            "tvq_attention_prefill_workspace": [vp, i64, i32, i64, i64, ctypes.POINTER(i64)],
+            "tvq_attention_prefill": [vp, vp, lay, i32, i64, i32, ctypes.c_float, ctypes.c_int, vp,
+                                      desc, ctypes.c_int, vp, desc, vp, i64, vp],
+            "tvq_attention_prefill_paged": [vp, vp, lay, vp, i32, vp, i64, vp, i32, i32,
+                                            ctypes.c_float, ctypes.c_int, vp, desc, ctypes.c_int,
+                                            vp, desc, vp, i64, vp],
+            "tvq_key_bounds_bytes": [vp, lay, ctypes.POINTER(i64)],
+            "tvq_key_bounds_paged": [vp, ctypes.c_int, vp, desc, vp, vp, i32, vp, lay, vp],
+            "tvq_select_blocks_workspace": [vp, i64, i64, i64, ctypes.POINTER(i64)],
+            "tvq_select_blocks": [vp, vp, lay, vp, i32, vp, i64, i64, i32, i32, ctypes.c_int, vp,
+                                  i32, i32, i32, vp, vp, vp, i64, vp],
+            "tvq_attention_blocks_workspace": [vp, i64, i32, i64, i64, ctypes.POINTER(i64)],
+            "tvq_attention_blocks": [vp, vp, lay, vp, i32, vp, i32, vp, i64, i32, i32,
+                                     ctypes.c_float, ctypes.c_int, vp, ctypes.c_int, vp, vp, i64,
+                                     vp]}.items():
+        f = getattr(L, name)
+        f.restype, f.argtypes = ctypes.c_int, args
     L.tvq_bits_per_element.restype = ctypes.c_double
     L.tvq_bits_per_element.argtypes = [vp, ctypes.c_int]
     L.tvq_status_string.restype = ctypes.c_char_p
@@ -261,6 +280,84 @@ def tvq_attention_paged(handle: int, pool_ptr: int, pool_lay: tvq_layout, table_
         num_q_heads, scale, q_dtype, q_ptr, o_dtype,
         o_ptr, ws_ptr, ws_bytes, stream),
         "tvq_attention_paged")
+
+
+def _bytes_of(name: str, *args) -> int:
+    out = ctypes.c_int64(0)
+    _check(getattr(load_library(), name)(*args, ctypes.byref(out)), name)
+    return int(out.value)
+
+
+def tvq_attention_prefill_workspace(handle: int, batch: int, num_q_heads: int, tokens: int,
+                                    max_ctx: int) -> int:
+    return _bytes_of("tvq_attention_prefill_workspace", handle, batch, num_q_heads, tokens, max_ctx)
+
+
+def tvq_attention_prefill(handle: int, cache_ptr: int, lay: tvq_layout, layer: int, t_end: int,
+                          num_q_heads: int, scale: float, q_dtype: int, q_ptr: int,
+                          q_desc: tvq_tensor_desc, o_dtype: int, o_ptr: int,
+                          o_desc: tvq_tensor_desc, ws_ptr: int, ws_bytes: int,
+                          stream: int = 0) -> None:
+    _check(load_library().tvq_attention_prefill(
+        handle, cache_ptr, ctypes.byref(lay), layer, t_end, num_q_heads, scale, q_dtype, q_ptr,
+        ctypes.byref(q_desc), o_dtype, o_ptr, ctypes.byref(o_desc), ws_ptr, ws_bytes, stream),
+        "tvq_attention_prefill")
+
+
+def tvq_attention_prefill_paged(handle: int, pool_ptr: int, pool_lay: tvq_layout, table_ptr: int,
+                                max_blocks: int, ctx_ptr: int, max_ctx: int, q_lens_ptr: int,
+                                layer: int, num_q_heads: int, scale: float, q_dtype: int,
+                                q_ptr: int, q_desc: tvq_tensor_desc, o_dtype: int, o_ptr: int,
+                                o_desc: tvq_tensor_desc, ws_ptr: int, ws_bytes: int,
+                                stream: int = 0) -> None:
+    _check(load_library().tvq_attention_prefill_paged(
+        handle, pool_ptr, ctypes.byref(pool_lay), table_ptr, max_blocks, ctx_ptr, max_ctx,
+        q_lens_ptr, layer, num_q_heads, scale, q_dtype, q_ptr, ctypes.byref(q_desc), o_dtype, o_ptr,
+        ctypes.byref(o_desc), ws_ptr, ws_bytes, stream), "tvq_attention_prefill_paged")
+
+
+def tvq_key_bounds_bytes(handle: int, pool_lay: tvq_layout) -> int:
+    return _bytes_of("tvq_key_bounds_bytes", handle, ctypes.byref(pool_lay))
+
+
+def tvq_key_bounds_paged(handle: int, in_dtype: int, k_ptr: int, desc: tvq_tensor_desc,
+                         positions_ptr: int, table_ptr: int, max_blocks: int, bounds_ptr: int,
+                         pool_lay: tvq_layout, stream: int = 0) -> None:
+    _check(load_library().tvq_key_bounds_paged(
+        handle, in_dtype, k_ptr, ctypes.byref(desc), positions_ptr, table_ptr, max_blocks,
+        bounds_ptr, ctypes.byref(pool_lay), stream), "tvq_key_bounds_paged")
+
+
+def tvq_select_blocks_workspace(handle: int, batch: int, max_ctx: int, block_tokens: int) -> int:
+    return _bytes_of("tvq_select_blocks_workspace", handle, batch, max_ctx, block_tokens)
+
+
+def tvq_select_blocks(handle: int, bounds_ptr: int, pool_lay: tvq_layout, table_ptr: int,
+                      max_blocks: int, ctx_ptr: int, max_ctx: int, batch: int, layer: int,
+                      num_q_heads: int, q_dtype: int, q_ptr: int, n_sel: int, n_first: int,
+                      n_last: int, blocks_ptr: int, lens_ptr: int, ws_ptr: int, ws_bytes: int,
+                      stream: int = 0) -> None:
+    _check(load_library().tvq_select_blocks(
+        handle, bounds_ptr, ctypes.byref(pool_lay), table_ptr, max_blocks, ctx_ptr, max_ctx, batch,
+        layer, num_q_heads, q_dtype, q_ptr, n_sel, n_first, n_last, blocks_ptr, lens_ptr, ws_ptr,
+        ws_bytes, stream), "tvq_select_blocks")
+
+
+def tvq_attention_blocks_workspace(handle: int, batch: int, num_q_heads: int, n_sel: int,
+                                   block_tokens: int) -> int:
+    return _bytes_of("tvq_attention_blocks_workspace", handle, batch, num_q_heads, n_sel,
+                     block_tokens)
+
+
+def tvq_attention_blocks(handle: int, pool_ptr: int, pool_lay: tvq_layout, table_ptr: int,
+                         max_blocks: int, blocks_ptr: int, n_sel: int, lens_ptr: int, batch: int,
+                         layer: int, num_q_heads: int, scale: float, q_dtype: int, q_ptr: int,
+                         o_dtype: int, o_ptr: int, ws_ptr: int, ws_bytes: int,
+                         stream: int = 0) -> None:
+    _check(load_library().tvq_attention_blocks(
+        handle, pool_ptr, ctypes.byref(pool_lay), table_ptr, max_blocks, blocks_ptr, n_sel, lens_ptr,
+        batch, layer, num_q_heads, scale, q_dtype, q_ptr, o_dtype, o_ptr, ws_ptr, ws_bytes, stream),
+        "tvq_attention_blocks")
 
 
 def tvq_bits_per_element(handle: int, accounting: int) -> float:

@@ -271,5 +271,175 @@ class Codec:
                               scale, dts[q.dtype], q.data_ptr(), dts[out.dtype], out.data_ptr(),
                               workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
 
+    # ---- many new tokens (tvq_attention_prefill / tvq_attention_prefill_paged) ----
+    def attention_prefill_workspace_bytes(self, batch: int, num_q_heads: int, tokens: int,
+                                          max_ctx: int) -> int:
+        return C.tvq_attention_prefill_workspace(self.handle, batch, num_q_heads, tokens, max_ctx)
+
+    def _check_rows(self, q, out) -> None:
+        if q.dim() != 4 or out.shape != q.shape or q.stride(-1) != 1 or out.stride(-1) != 1:
+            raise ValueError("q and out must be [B, Hq, T, d] GPU tensors with d contiguous")
+        if q.shape[3] != self.d:
+            raise ValueError(f"q has head dim {q.shape[3]}, the codec {self.d}")
+
+    @staticmethod
+    def _io_dtypes(q, out):
+        import torch
+        dts = {torch.bfloat16: C.TVQ_BF16, torch.float32: C.TVQ_F32}
+        if q.dtype not in dts or out.dtype not in dts:
+            raise ValueError("q/out must be bf16 or fp32")
+        return dts[q.dtype], dts[out.dtype]
+
+    @staticmethod
+    def _rows_desc(t) -> C.tvq_tensor_desc:
+        s = t.stride()
+        return C.tvq_tensor_desc(t.shape[0], t.shape[2], 0, s[0], s[1], s[2])
+
+    @staticmethod
+    def _workspace(workspace, need, device):
+        """The given workspace (the call itself checks its size) or a new one of need() bytes."""
+        import torch
+        if workspace is None:
+            return torch.empty(need(), dtype=torch.uint8, device=device)
+        if workspace.dtype != torch.uint8 or not workspace.is_cuda or \
+                not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous uint8 GPU tensor")
+        return workspace
+
+    def attention_prefill(self, cache, lay: C.tvq_layout, layer: int, t_end: int, q, out,
+                          scale: float, workspace=None, stream=None) -> None:
+        """Causal attention of the newest T tokens of every sequence, q [B, Hq, T, d] (any strides
+        with d contiguous), into out: token j stands at position t_end - T + j and attends to the
+        positions up to its own."""
+        self._check_rows(q, out)
+        _check_bytes(cache, lay, "cache")
+        _on_gpu(q, out, cache)
+        dq, do = self._io_dtypes(q, out)
+        B, Hq, T, _ = q.shape
+        workspace = self._workspace(
+            workspace, lambda: self.attention_prefill_workspace_bytes(B, Hq, T, t_end), q.device)
+        C.tvq_attention_prefill(self.handle, cache.data_ptr(), lay, layer, t_end, Hq, scale, dq,
+                                q.data_ptr(), self._rows_desc(q), do, out.data_ptr(),
+                                self._rows_desc(out), workspace.data_ptr(), workspace.numel(),
+                                _stream_handle(stream))
+
+    def attention_prefill_paged(self, pool, pool_lay: C.tvq_layout, block_table, ctx_lens,
+                                max_ctx: int, layer: int, q, out, scale: float, q_lens=None,
+                                workspace=None, stream=None) -> None:
+        """attention_prefill over a paged pool: sequence b has q_lens[b] new tokens (all T without
+        q_lens; rows behind them are not written), the last at position ctx_lens[b] - 1."""
+        self._check_rows(q, out)
+        _check_bytes(pool, pool_lay, "pool")
+        _on_gpu(q, out, pool, block_table, ctx_lens)
+        dq, do = self._io_dtypes(q, out)
+        B, Hq, T, _ = q.shape
+        if block_table.dim() != 2 or block_table.shape[0] != B or ctx_lens.shape != (B,) or \
+                (q_lens is not None and q_lens.shape != (B,)):
+            raise ValueError("block_table [B, max_blocks], ctx_lens [B] and q_lens [B] must match q")
+        workspace = self._workspace(
+            workspace, lambda: self.attention_prefill_workspace_bytes(B, Hq, T, max_ctx), q.device)
+        C.tvq_attention_prefill_paged(self.handle, pool.data_ptr(), pool_lay,
+                                      self._i32(block_table, "block_table"), block_table.shape[1],
+                                      self._i32(ctx_lens, "ctx_lens"), max_ctx,
+                                      0 if q_lens is None else self._i32(q_lens, "q_lens"), layer,
+                                      Hq, scale, dq, q.data_ptr(), self._rows_desc(q), do,
+                                      out.data_ptr(), self._rows_desc(out), workspace.data_ptr(),
+                                      workspace.numel(), _stream_handle(stream))
+
+    # ---- part of a long context (tvq_key_bounds_paged / tvq_select_blocks / tvq_attention_blocks)
+    def alloc_key_bounds(self, pool_lay: C.tvq_layout, device="cuda"):
+        """Room for the key bounds of a pool, [L, n_blocks, H, 2, d] bf16 (lo, hi)."""
+        import torch
+        C.tvq_key_bounds_bytes(self.handle, pool_lay)        # refuses another codec's layout
+        return torch.empty((self.L, pool_lay.batch, self.H, 2, self.d), dtype=torch.bfloat16,
+                           device=device)
+
+    def _check_bounds(self, bounds, pool_lay: C.tvq_layout) -> None:
+        import torch
+        want = (self.L, pool_lay.batch, self.H, 2, self.d)
+        if bounds.dtype != torch.bfloat16 or not bounds.is_contiguous() or \
+                tuple(bounds.shape) != want:
+            raise ValueError(f"bounds must be a contiguous bf16 GPU tensor of shape {want}")
+
+    def key_bounds_paged(self, k, positions, block_table, bounds, pool_lay: C.tvq_layout,
+                         stream=None) -> None:
+        """Bring the key bounds of the pool's blocks up to date with the keys of an encode_paged
+        call (the same k, positions and block_table)."""
+        import torch
+        dt = {torch.bfloat16: C.TVQ_BF16, torch.float32: C.TVQ_F32}.get(k.dtype)
+        if dt is None:
+            raise ValueError("k must be bf16 or fp32")
+        self._check_kv(k, "k")
+        self._check_bounds(bounds, pool_lay)
+        _on_gpu(k, bounds)
+        if block_table.dim() != 2 or positions.shape != (k.shape[1],) or \
+                block_table.shape[0] != k.shape[1]:
+            raise ValueError("positions [B] and block_table [B, max_blocks] must match k")
+        C.tvq_key_bounds_paged(self.handle, dt, k.data_ptr(), desc_of(k),
+                               self._i32(positions, "positions"),
+                               self._i32(block_table, "block_table"), block_table.shape[1],
+                               bounds.data_ptr(), pool_lay, _stream_handle(stream))
+
+    def select_blocks_workspace_bytes(self, batch: int, max_ctx: int, block_tokens: int) -> int:
+        return C.tvq_select_blocks_workspace(self.handle, batch, max_ctx, block_tokens)
+
+    def select_blocks(self, bounds, pool_lay: C.tvq_layout, block_table, ctx_lens, max_ctx: int,
+                      layer: int, q, blocks, sel_lens, n_first: int = 1, n_last: int = 1,
+                      workspace=None, stream=None) -> None:
+        """For q ([B, Hq, d]) and each KV head, the blocks of the context whose keys can score
+        highest, into blocks ([B, H, n_sel] int32, ascending, -1 behind them) and their tokens into
+        sel_lens ([B, H] int32).  The first n_first and last n_last blocks are always among them."""
+        import torch
+        if q.dim() != 3 or not q.is_contiguous() or q.shape[2] != self.d:
+            raise ValueError(f"q must be a contiguous [B, Hq, {self.d}] GPU tensor")
+        self._check_bounds(bounds, pool_lay)
+        _on_gpu(q, bounds, block_table, ctx_lens, blocks, sel_lens)
+        dt = {torch.bfloat16: C.TVQ_BF16, torch.float32: C.TVQ_F32}.get(q.dtype)
+        if dt is None:
+            raise ValueError("q must be bf16 or fp32")
+        B = q.shape[0]
+        if block_table.dim() != 2 or block_table.shape[0] != B or ctx_lens.shape != (B,):
+            raise ValueError("block_table [B, max_blocks] and ctx_lens [B] must match q")
+        if blocks.dim() != 3 or blocks.shape[:2] != (B, self.H) or sel_lens.shape != (B, self.H):
+            raise ValueError("blocks [B, H, n_sel] and sel_lens [B, H] must match q and the codec")
+        workspace = self._workspace(
+            workspace, lambda: self.select_blocks_workspace_bytes(B, max_ctx,
+                                                                  pool_lay.capacity_tokens), q.device)
+        C.tvq_select_blocks(self.handle, bounds.data_ptr(), pool_lay,
+                            self._i32(block_table, "block_table"), block_table.shape[1],
+                            self._i32(ctx_lens, "ctx_lens"), max_ctx, B, layer, q.shape[1], dt,
+                            q.data_ptr(), blocks.shape[2], n_first, n_last,
+                            self._i32(blocks, "blocks"), self._i32(sel_lens, "sel_lens"),
+                            workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
+
+    def attention_blocks_workspace_bytes(self, batch: int, num_q_heads: int, n_sel: int,
+                                         block_tokens: int) -> int:
+        return C.tvq_attention_blocks_workspace(self.handle, batch, num_q_heads, n_sel,
+                                                block_tokens)
+
+    def attention_blocks(self, pool, pool_lay: C.tvq_layout, block_table, blocks, sel_lens,
+                         layer: int, q, out, scale: float, workspace=None, stream=None) -> None:
+        """Attention of q ([B, Hq, d]) over listed blocks: KV head h of sequence b attends to the
+        first sel_lens[b, h] slots of blocks[b, h, 0], blocks[b, h, 1], ..."""
+        self._check_q(q, out)
+        _check_bytes(pool, pool_lay, "pool")
+        _on_gpu(q, out, pool, block_table, blocks, sel_lens)
+        dq, do = self._io_dtypes(q, out)
+        B, Hq, _ = q.shape
+        if block_table.dim() != 2 or block_table.shape[0] != B:
+            raise ValueError("block_table [B, max_blocks] must match q")
+        if blocks.dim() != 3 or blocks.shape[:2] != (B, self.H) or sel_lens.shape != (B, self.H):
+            raise ValueError("blocks [B, H, n_sel] and sel_lens [B, H] must match q and the codec")
+        n_sel = blocks.shape[2]
+        workspace = self._workspace(
+            workspace, lambda: self.attention_blocks_workspace_bytes(B, Hq, n_sel,
+                                                                     pool_lay.capacity_tokens),
+            q.device)
+        C.tvq_attention_blocks(self.handle, pool.data_ptr(), pool_lay,
+                               self._i32(block_table, "block_table"), block_table.shape[1],
+                               self._i32(blocks, "blocks"), n_sel, self._i32(sel_lens, "sel_lens"),
+                               B, layer, Hq, scale, dq, q.data_ptr(), do, out.data_ptr(),
+                               workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
+
     def bits_per_element(self, accounting: int = 0) -> float:
         return C.tvq_bits_per_element(self.handle, accounting)

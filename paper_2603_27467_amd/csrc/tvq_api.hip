@@ -15,7 +15,9 @@
 #include <vector>
 
 #include "../../include/tvq.h"
+#include "tvq_bounds.h"
 #include "tvq_internal.h"
+#include "tvq_rows.h"
 #include "tvq_spans.h"
 
 struct tvq_codec {
@@ -26,6 +28,7 @@ struct tvq_codec {
   std::vector<tvq::SegParams> segs;          // [2L]
   uint64_t rec_total = 0;                    // record bytes of all planes, per slot
   int device = 0;
+  int n_cu = 0;                              // its compute units
   void* scratch = nullptr;                   // the static attention scratch on `device`
   // waves of the attention kernel that the device holds at once (d = 64, 128), per key and value
   // format (bit 0: 8-bit angle codes, bit 1: 4-bit log norms), and the most over the formats
@@ -497,6 +500,7 @@ tvq_status tvq_create(const tvq_config* cfg, tvq_codec** out) {
         c->attn_slots[kf][vf] = (int64_t)n_cu * blocks * tvq::kWavesPerBlock;
         c->attn_slots_max = std::max(c->attn_slots_max, c->attn_slots[kf][vf]);
       }
+    c->n_cu = n_cu;
   }
   // segment lists of the two decode kernels
   std::vector<uint32_t> lists;
@@ -1009,6 +1013,298 @@ tvq_status tvq_attention_paged(const tvq_codec* c, const void* pool, const tvq_l
   return attention_launch(c, a, pool, pool_layout, batch, layer, max_ctx,
                           pool_layout->capacity_tokens, num_q_heads, scale, q_dtype, q, o_dtype, o,
                           workspace, workspace_bytes, stream);
+}
+
+// Query heads per KV head of a call, or 0 where they do not divide or are too many.
+static uint32_t group_of(const tvq_codec* c, int32_t num_q_heads) {
+  if (num_q_heads < c->H || num_q_heads % c->H != 0) return 0;
+  const uint32_t g = (uint32_t)(num_q_heads / c->H);
+  return g <= tvq::kAttnMaxGroup ? g : 0u;
+}
+
+static tvq_status group_status(const tvq_codec* c, int32_t num_q_heads) {
+  if (group_of(c, num_q_heads)) return TVQ_OK;
+  return num_q_heads >= c->H && num_q_heads % c->H == 0 ? TVQ_ERR_UNSUPPORTED
+                                                        : TVQ_ERR_INVALID_ARG;
+}
+
+static bool is_dtype(tvq_dtype t) { return t == TVQ_BF16 || t == TVQ_F32; }
+
+// The plan of a call of many query rows; false where its counts leave the kernels' ranges.
+static bool rows_plan_of(const tvq_codec* c, int64_t batch, int64_t rows, int64_t tokens,
+                         tvq::RowsPlan* p) {
+  if (batch < 1 || rows < 1 || tokens < 1 || tokens >= (1ll << 31) || rows >= (1ll << 31) ||
+      batch >= (1ll << 31) / c->H || batch * c->H * rows >= (1ll << 31))
+    return false;
+  *p = tvq::rows_plan(batch, c->H, rows, tokens, c->d, c->n_cu);
+  return p->units * p->n_split < (1ll << 31) && p->units * p->unit_rows < (1ll << 31);
+}
+
+// The shared body of the entry points over many query rows: `a` holds the paging, list and lengths.
+static tvq_status rows_launch(const tvq_codec* c, tvq::RowsArgs& a, const void* cache,
+                              const tvq_layout* lay, int64_t batch, int64_t tokens, int64_t t_end,
+                              int32_t layer, int32_t num_q_heads, float scale, tvq_dtype q_dtype,
+                              const void* q, const int64_t (&q_stride)[3], tvq_dtype o_dtype,
+                              void* o, const int64_t (&o_stride)[3], void* workspace,
+                              int64_t workspace_bytes, void* stream) {
+  if (layer < 0 || layer >= c->L) return TVQ_ERR_INVALID_ARG;
+  if (!is_dtype(q_dtype) || !is_dtype(o_dtype)) return TVQ_ERR_INVALID_ARG;
+  if (!(scale == scale) || scale > 3.0e38f || scale < -3.0e38f) return TVQ_ERR_INVALID_ARG;
+  const tvq_status st = group_status(c, num_q_heads);
+  if (st != TVQ_OK) return st;
+  const int64_t G = group_of(c, num_q_heads);
+  for (int kind = 0; kind < 2; ++kind) {
+    const tvq::SegParams& sp = c->segs[2 * layer + kind];
+    if (!tvq::fast_format(sp.n, sp.mode, sp.bits)) return TVQ_ERR_UNSUPPORTED;
+  }
+  tvq::RowsPlan p;
+  if (!rows_plan_of(c, batch, tokens * G, t_end, &p)) return TVQ_ERR_INVALID_ARG;
+  if (!cache || !q || !o || !aligned16(cache) || !aligned16(q) || !aligned16(o))
+    return TVQ_ERR_INVALID_ARG;
+  if (p.ws_bytes > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < p.ws_bytes))
+    return TVQ_ERR_INVALID_ARG;
+  const int64_t n_slots = lay->batch * c->H * lay->capacity_tokens;
+  for (int kind = 0; kind < 2; ++kind) {
+    const tvq::SegParams& sp = c->segs[2 * layer + kind];
+    a.n[kind] = sp.n;
+    a.log_norms[kind] = sp.mode == TVQ_NORM_LOG ? 1u : 0u;
+    a.lut[kind] = c->d_lut + 2 * (size_t)sp.lut_off;
+    for (int k = 0; k < 3; ++k)
+      a.plane[kind][k] = (const uint8_t*)cache + n_slots * (int64_t)sp.pre[k];
+  }
+  a.signs = c->d_sign_masks + (size_t)layer * (c->d / 2);
+  a.B = (uint32_t)batch;
+  a.H = (uint32_t)c->H;
+  a.G = (uint32_t)G;
+  a.T = (uint32_t)tokens;
+  a.t_end = (uint32_t)t_end;
+  a.cap = (uint32_t)lay->capacity_tokens;
+  a.n_rb = p.n_rb;
+  a.n_split = p.n_split;
+  a.min_tiles = p.min_tiles;
+  a.tile = p.tile;
+  a.unit_rows = p.unit_rows;
+  a.q_f32 = q_dtype == TVQ_F32 ? 1u : 0u;
+  a.o_f32 = o_dtype == TVQ_F32 ? 1u : 0u;
+  a.qscale = scale * 1.4426950408889634f;          // scores in log2 units
+  a.q = q;
+  a.o = o;
+  for (int k = 0; k < 3; ++k) a.q_stride[k] = q_stride[k], a.o_stride[k] = o_stride[k];
+  a.ws_acc = (float*)workspace;
+  a.ws_ml = p.ws_bytes > 0 ? (float*)((char*)workspace + p.acc_bytes) : nullptr;
+  const int rc = tvq_launch_rows(a, c->d, p.waves, o_dtype == TVQ_F32, stream);
+  if (rc == -1) return TVQ_ERR_UNSUPPORTED;
+  return rc == 0 ? TVQ_OK : TVQ_ERR_HIP;
+}
+
+// A [B][num_q_heads][T][d] view: as desc_valid, with the query heads in the place of the heads.
+static bool rows_desc_valid(const tvq_codec* c, const tvq_tensor_desc* t, int32_t num_q_heads,
+                            tvq_dtype dtype, bool written) {
+  if (!t || t->batch < 1 || t->tokens < 0 || num_q_heads < 1 || !is_dtype(dtype)) return false;
+  const int64_t strides[3] = {t->stride_b, t->stride_h, t->stride_t};
+  const int64_t sizes[3] = {t->batch, num_q_heads, t->tokens};
+  const int64_t eb = dtype == TVQ_F32 ? 4 : 2;
+  for (int i = 0; i < 3; ++i) {
+    if (strides[i] < 0 || strides[i] >= (1ll << 40) || (strides[i] * eb) % 16 != 0) return false;
+    if (sizes[i] >= (1ll << 31)) return false;
+    if (written && sizes[i] > 1 && strides[i] < c->d) return false;
+  }
+  return true;
+}
+
+static tvq_status prefill_launch(const tvq_codec* c, tvq::RowsArgs& a, const void* cache,
+                                 const tvq_layout* lay, int64_t t_end, int32_t layer,
+                                 int32_t num_q_heads, float scale, tvq_dtype q_dtype, const void* q,
+                                 const tvq_tensor_desc* qd, tvq_dtype o_dtype, void* o,
+                                 const tvq_tensor_desc* od, void* workspace,
+                                 int64_t workspace_bytes, void* stream) {
+  if (!rows_desc_valid(c, qd, num_q_heads, q_dtype, false) ||
+      !rows_desc_valid(c, od, num_q_heads, o_dtype, true) || qd->batch != od->batch ||
+      qd->tokens != od->tokens || t_end < 1)
+    return TVQ_ERR_INVALID_ARG;
+  if (qd->tokens == 0) return TVQ_OK;
+  const int64_t qs[3] = {qd->stride_b, qd->stride_h, qd->stride_t};
+  const int64_t os[3] = {od->stride_b, od->stride_h, od->stride_t};
+  return rows_launch(c, a, cache, lay, qd->batch, qd->tokens, t_end, layer, num_q_heads, scale,
+                     q_dtype, q, qs, o_dtype, o, os, workspace, workspace_bytes, stream);
+}
+
+tvq_status tvq_attention_prefill_workspace(const tvq_codec* c, int64_t batch, int32_t num_q_heads,
+                                           int64_t tokens, int64_t max_ctx, int64_t* bytes) {
+  if (!c || !bytes || tokens < 0 || tokens >= (1ll << 31)) return TVQ_ERR_INVALID_ARG;
+  const tvq_status st = group_status(c, num_q_heads);
+  if (st != TVQ_OK) return st;
+  tvq::RowsPlan p;
+  if (!rows_plan_of(c, batch, std::max<int64_t>(tokens, 1) * group_of(c, num_q_heads), max_ctx, &p))
+    return TVQ_ERR_INVALID_ARG;
+  *bytes = p.ws_bytes;
+  return TVQ_OK;
+}
+
+tvq_status tvq_attention_prefill(const tvq_codec* c, const void* cache, const tvq_layout* lay,
+                                 int32_t layer, int64_t t_end, int32_t num_q_heads, float scale,
+                                 tvq_dtype q_dtype, const void* q, const tvq_tensor_desc* q_desc,
+                                 tvq_dtype o_dtype, void* o, const tvq_tensor_desc* o_desc,
+                                 void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!c || !lay || !layout_matches(c, lay) || !q_desc || q_desc->batch != lay->batch)
+    return TVQ_ERR_INVALID_ARG;
+  if (t_end > lay->capacity_tokens || q_desc->tokens > t_end) return TVQ_ERR_INVALID_ARG;
+  tvq::RowsArgs a;
+  std::memset(&a, 0, sizeof(a));
+  return prefill_launch(c, a, cache, lay, t_end, layer, num_q_heads, scale, q_dtype, q, q_desc,
+                        o_dtype, o, o_desc, workspace, workspace_bytes, stream);
+}
+
+tvq_status tvq_attention_prefill_paged(const tvq_codec* c, const void* pool,
+                                       const tvq_layout* pool_layout, const int32_t* block_table,
+                                       int32_t max_blocks, const int32_t* ctx_lens,
+                                       int64_t max_ctx, const int32_t* q_lens, int32_t layer,
+                                       int32_t num_q_heads, float scale, tvq_dtype q_dtype,
+                                       const void* q, const tvq_tensor_desc* q_desc,
+                                       tvq_dtype o_dtype, void* o, const tvq_tensor_desc* o_desc,
+                                       void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!c) return TVQ_ERR_INVALID_ARG;
+  tvq::RowsArgs a;
+  std::memset(&a, 0, sizeof(a));
+  if (!paging_valid(c, pool_layout, block_table, max_blocks, &a.pg)) return TVQ_ERR_INVALID_ARG;
+  if (!ctx_lens || ((uintptr_t)ctx_lens & 3u) != 0 || ((uintptr_t)q_lens & 3u) != 0)
+    return TVQ_ERR_INVALID_ARG;
+  if (max_ctx > (int64_t)max_blocks * pool_layout->capacity_tokens) return TVQ_ERR_INVALID_ARG;
+  a.pg.seq = ctx_lens;
+  a.q_lens = q_lens;
+  return prefill_launch(c, a, pool, pool_layout, max_ctx, layer, num_q_heads, scale, q_dtype, q,
+                        q_desc, o_dtype, o, o_desc, workspace, workspace_bytes, stream);
+}
+
+tvq_status tvq_key_bounds_bytes(const tvq_codec* c, const tvq_layout* pool_layout, int64_t* bytes) {
+  if (!c || !bytes || !layout_matches(c, pool_layout)) return TVQ_ERR_INVALID_ARG;
+  *bytes = (int64_t)c->L * pool_layout->batch * c->H * 4 * c->d;
+  return TVQ_OK;
+}
+
+tvq_status tvq_key_bounds_paged(const tvq_codec* c, tvq_dtype in_dtype, const void* k,
+                                const tvq_tensor_desc* in, const int32_t* positions,
+                                const int32_t* block_table, int32_t max_blocks, void* bounds,
+                                const tvq_layout* pool_layout, void* stream) {
+  if (!c || !in || !is_dtype(in_dtype)) return TVQ_ERR_INVALID_ARG;
+  if (!desc_valid(c, in, in_dtype == TVQ_F32 ? 4 : 2)) return TVQ_ERR_INVALID_ARG;
+  tvq::KeyBoundsArgs a;
+  std::memset(&a, 0, sizeof(a));
+  if (!paging_valid(c, pool_layout, block_table, max_blocks, &a.pg)) return TVQ_ERR_INVALID_ARG;
+  if (!positions || ((uintptr_t)positions & 3u) != 0) return TVQ_ERR_INVALID_ARG;
+  if (in->tokens == 0) return TVQ_OK;
+  if (!k || !bounds || !aligned16(k) || !aligned16(bounds)) return TVQ_ERR_INVALID_ARG;
+  const int64_t bt = pool_layout->capacity_tokens;
+  const int64_t touch = (in->tokens + bt - 2) / bt + 1;   // blocks that a sequence's tokens may touch
+  if ((int64_t)c->L * in->batch * touch * c->H >= (1ll << 31)) return TVQ_ERR_INVALID_ARG;
+  a.k = k;
+  a.stride_l = in->stride_l;
+  a.stride_b = (uint32_t)in->stride_b;
+  a.stride_h = (uint32_t)in->stride_h;
+  a.stride_t = (uint32_t)in->stride_t;
+  a.L = (uint32_t)c->L;
+  a.B = (uint32_t)in->batch;
+  a.H = (uint32_t)c->H;
+  a.T = (uint32_t)in->tokens;
+  a.n_touch = (uint32_t)touch;
+  a.pg.seq = positions;
+  a.bounds = (uint16_t*)bounds;
+  const int rc = tvq_launch_key_bounds(a, c->d, in_dtype == TVQ_F32, stream);
+  if (rc == -1) return TVQ_ERR_UNSUPPORTED;
+  return rc == 0 ? TVQ_OK : TVQ_ERR_HIP;
+}
+
+static bool block_tokens_valid(int64_t bt) {
+  return bt >= 32 && bt <= 65536 && (bt & (bt - 1)) == 0;
+}
+
+tvq_status tvq_select_blocks_workspace(const tvq_codec* c, int64_t batch, int64_t max_ctx,
+                                       int64_t block_tokens, int64_t* bytes) {
+  if (!c || !bytes || batch < 1 || batch >= (1ll << 31) / c->H || max_ctx < 1 ||
+      max_ctx >= (1ll << 31) || !block_tokens_valid(block_tokens))
+    return TVQ_ERR_INVALID_ARG;
+  const int64_t n_keys = (max_ctx + block_tokens - 1) / block_tokens;
+  if (batch * c->H * n_keys >= (1ll << 31)) return TVQ_ERR_INVALID_ARG;
+  *bytes = batch * c->H * n_keys * 4;
+  return TVQ_OK;
+}
+
+tvq_status tvq_select_blocks(const tvq_codec* c, const void* bounds, const tvq_layout* pool_layout,
+                             const int32_t* block_table, int32_t max_blocks,
+                             const int32_t* ctx_lens, int64_t max_ctx, int64_t batch,
+                             int32_t layer, int32_t num_q_heads, tvq_dtype q_dtype, const void* q,
+                             int32_t n_sel, int32_t n_first, int32_t n_last, int32_t* blocks,
+                             int32_t* sel_lens, void* workspace, int64_t workspace_bytes,
+                             void* stream) {
+  if (!c || layer < 0 || layer >= c->L || !is_dtype(q_dtype)) return TVQ_ERR_INVALID_ARG;
+  tvq::SelectArgs a;
+  std::memset(&a, 0, sizeof(a));
+  if (!paging_valid(c, pool_layout, block_table, max_blocks, &a.pg)) return TVQ_ERR_INVALID_ARG;
+  if (!ctx_lens || ((uintptr_t)ctx_lens & 3u) != 0) return TVQ_ERR_INVALID_ARG;
+  if (max_ctx > (int64_t)max_blocks * pool_layout->capacity_tokens) return TVQ_ERR_INVALID_ARG;
+  tvq_status st = group_status(c, num_q_heads);
+  if (st != TVQ_OK) return st;
+  if (n_first < 0 || n_last < 1 || n_sel > 65536 || (int64_t)n_first + n_last > n_sel)
+    return TVQ_ERR_INVALID_ARG;
+  int64_t need = 0;
+  st = tvq_select_blocks_workspace(c, batch, max_ctx, pool_layout->capacity_tokens, &need);
+  if (st != TVQ_OK) return st;
+  if (!bounds || !q || !blocks || !sel_lens || !workspace || !aligned16(bounds) || !aligned16(q) ||
+      ((uintptr_t)blocks & 3u) != 0 || ((uintptr_t)sel_lens & 3u) != 0 || !aligned16(workspace) ||
+      workspace_bytes < need)
+    return TVQ_ERR_INVALID_ARG;
+  a.bounds = (const uint16_t*)bounds + (size_t)layer * pool_layout->batch * c->H * 2 * c->d;
+  a.q = q;
+  a.pg.seq = ctx_lens;
+  a.B = (uint32_t)batch;
+  a.H = (uint32_t)c->H;
+  a.G = group_of(c, num_q_heads);
+  a.max_ctx = (uint32_t)max_ctx;
+  a.n_keys = (uint32_t)(need / 4 / (batch * c->H));
+  a.n_sel = (uint32_t)n_sel;
+  a.n_first = (uint32_t)n_first;
+  a.n_last = (uint32_t)n_last;
+  a.keys = (uint32_t*)workspace;
+  a.blocks = blocks;
+  a.lens = sel_lens;
+  const int rc = tvq_launch_select(a, c->d, q_dtype == TVQ_F32, stream);
+  if (rc == -1) return TVQ_ERR_UNSUPPORTED;
+  return rc == 0 ? TVQ_OK : TVQ_ERR_HIP;
+}
+
+tvq_status tvq_attention_blocks_workspace(const tvq_codec* c, int64_t batch, int32_t num_q_heads,
+                                          int64_t n_sel, int64_t block_tokens, int64_t* bytes) {
+  if (!c || !bytes || n_sel < 1 || n_sel >= (1ll << 31) || !block_tokens_valid(block_tokens))
+    return TVQ_ERR_INVALID_ARG;
+  const tvq_status st = group_status(c, num_q_heads);
+  if (st != TVQ_OK) return st;
+  tvq::RowsPlan p;
+  if (!rows_plan_of(c, batch, group_of(c, num_q_heads), n_sel * block_tokens, &p))
+    return TVQ_ERR_INVALID_ARG;
+  *bytes = p.ws_bytes;
+  return TVQ_OK;
+}
+
+tvq_status tvq_attention_blocks(const tvq_codec* c, const void* pool, const tvq_layout* pool_layout,
+                                const int32_t* block_table, int32_t max_blocks,
+                                const int32_t* blocks, int32_t n_sel, const int32_t* sel_lens,
+                                int64_t batch, int32_t layer, int32_t num_q_heads, float scale,
+                                tvq_dtype q_dtype, const void* q, tvq_dtype o_dtype, void* o,
+                                void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!c) return TVQ_ERR_INVALID_ARG;
+  tvq::RowsArgs a;
+  std::memset(&a, 0, sizeof(a));
+  if (!paging_valid(c, pool_layout, block_table, max_blocks, &a.pg)) return TVQ_ERR_INVALID_ARG;
+  if (!blocks || !sel_lens || ((uintptr_t)blocks & 3u) != 0 || ((uintptr_t)sel_lens & 3u) != 0 ||
+      n_sel < 1)
+    return TVQ_ERR_INVALID_ARG;
+  a.pg.seq = sel_lens;
+  a.list = blocks;
+  a.n_list = (uint32_t)n_sel;
+  const int64_t s[3] = {(int64_t)num_q_heads * c->d, c->d, c->d};
+  return rows_launch(c, a, pool, pool_layout, batch, 1, n_sel * pool_layout->capacity_tokens, layer,
+                     num_q_heads, scale, q_dtype, q, s, o_dtype, o, s, workspace, workspace_bytes,
+                     stream);
 }
 
 double tvq_bits_per_element_config(const tvq_config* cfg, int accounting) {

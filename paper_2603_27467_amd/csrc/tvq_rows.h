@@ -1,0 +1,102 @@
+// tvq_rows.h -- attention of many query rows over the codes (tvq_rows.hip): its arguments, and how
+// a call is split over workgroups.  The split is plain arithmetic, compiled into the library and,
+// by itself, into the host tests.
+//
+// The query rows of one (sequence, KV head) are its new tokens times the G query heads, row r =
+// token r / G, head r % G.  A unit is a block of consecutive rows of one (sequence, KV head) that
+// a workgroup takes; the tokens that a unit attends to are cut into spans of whole tiles, one per
+// workgroup, whose partials are merged.
+#pragma once
+
+#include <stdint.h>
+
+#include "tvq_internal.h"
+
+#if defined(__HIPCC__)
+#define TVQ_ROWS_HOST_DEVICE __host__ __device__ __forceinline__
+#else
+#define TVQ_ROWS_HOST_DEVICE inline
+#endif
+
+namespace tvq {
+
+struct RowsArgs {
+  Paging pg;             // pg.seq: context lengths, or tokens per (sequence, KV head) with a list
+  const int32_t* list;   // [B][H][n_list] block numbers of the sequence (nullptr: all in order)
+  uint32_t n_list;
+  const int32_t* q_lens; // new tokens per sequence (nullptr: T)
+  uint32_t B, H, G, T;   // T: token rows of q and o
+  uint32_t t_end;        // bound of every context
+  uint32_t cap;          // capacity tokens of a contiguous cache
+  uint32_t n_rb;         // units of a (sequence, KV head)
+  uint32_t n_split;      // most spans of a unit
+  uint32_t min_tiles;    // fewest tiles of a span where a unit has several
+  uint32_t tile;         // tokens of a tile
+  uint32_t unit_rows;    // rows of a unit
+  uint32_t q_f32, o_f32;
+  float qscale;          // scale * log2(e): scores in log2 units
+  const void* q;
+  void* o;
+  int64_t q_stride[3], o_stride[3];   // elements, of sequence, query head and token
+  const uint32_t* signs;
+  const float* lut[2];   // K and V tables: float2 entries, 1/sqrt(d) folded in
+  uint32_t n[2];         // angle bins: 64, 128 or 256
+  uint32_t log_norms[2]; // 4-bit log-space norms, else 8-bit linear
+  const uint8_t* plane[2][3];
+  float* ws_acc;         // [unit][span][unit_rows][d]
+  float* ws_ml;          // [unit][span][unit_rows][2]
+};
+
+// Spans that a unit of `tiles` tiles is cut into.
+TVQ_ROWS_HOST_DEVICE uint32_t row_spans(uint32_t tiles, uint32_t n_split, uint32_t min_tiles) {
+  const uint32_t most = tiles / min_tiles;
+  const uint32_t n = most < n_split ? most : n_split;
+  return n < 1u ? 1u : n;
+}
+
+// First tile of span k of n.
+TVQ_ROWS_HOST_DEVICE uint32_t span_start(uint32_t tiles, uint32_t n, uint32_t k) {
+  const uint32_t per = tiles / n, extra = tiles - per * n;
+  return k * per + (k < extra ? k : extra);
+}
+
+struct RowsPlan {
+  uint32_t waves;        // of a workgroup: 1 or 4
+  uint32_t unit_rows, tile, n_rb, n_split, min_tiles;
+  int64_t units, acc_bytes, ws_bytes;
+};
+
+// batch, heads: of the cache; rows: query rows of a (sequence, KV head); tokens: bound of a
+// context; d: head dimension; cus: compute units.
+//
+// Up to 32 rows a wave works by itself, with its own tile in LDS; above, four waves share a tile.
+// The spans of a launch fill the places that the device has for its workgroups (8 single waves or 2
+// workgroups of four a compute unit), of at least 128 or 256 tokens each, so that a span's start
+// and its partial stay small beside it.
+inline RowsPlan rows_plan(int64_t batch, int64_t heads, int64_t rows, int64_t tokens, int32_t d,
+                          int64_t cus) {
+  const auto ceil_div = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  RowsPlan p;
+  p.waves = rows <= 32 ? 1 : 4;
+  p.unit_rows = p.waves * 32;
+  p.tile = p.waves == 1 ? 32 : 64;
+  p.min_tiles = 4;
+  const int64_t n_rb = ceil_div(rows, p.unit_rows);
+  p.n_rb = (uint32_t)n_rb;
+  p.units = batch * heads * n_rb;
+  const int64_t places = cus * (p.waves == 1 ? 8 : 2);
+  int64_t n = ceil_div(places, p.units);
+  const int64_t most = tokens / (p.min_tiles * (int64_t)p.tile);
+  n = n < most ? n : most;
+  p.n_split = (uint32_t)(n < 1 ? 1 : n);
+  const int64_t parts = p.n_split > 1 ? p.units * p.n_split * p.unit_rows : 0;
+  p.acc_bytes = (parts * d * 4 + 255) / 256 * 256;
+  p.ws_bytes = p.acc_bytes + parts * 8;
+  return p;
+}
+
+}  // namespace tvq
+
+#if defined(__HIPCC__)
+int tvq_launch_rows(const tvq::RowsArgs& a, int d, unsigned waves, bool wide, void* stream);
+#endif
