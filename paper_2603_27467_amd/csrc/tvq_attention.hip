@@ -64,18 +64,6 @@ struct AttnWave {
   uint32_t blk;                  // paged: lane i holds the pool block of the wave's i-th block
 };
 
-// Inclusive prefix sum over the wave's lanes (row shifts inside the rows of 16, then the last
-// lane of each row or half broadcast to the next; lanes without a source add 0).
-__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);
-  return v;
-}
-
 // Context of sequence b: t_end, or its own length clipped to it.
 __device__ __forceinline__ uint32_t seq_context(const AttnArgs& a, uint32_t b) {
   if (!a.pg.seq) return a.t_end;

@@ -18,6 +18,7 @@
 #include "tvq_bounds.h"
 #include "tvq_device.h"
 #include "tvq_internal.h"
+#include "tvq_lanes.h"
 
 namespace tvq {
 namespace {
@@ -144,6 +145,10 @@ __global__ __launch_bounds__(kBlockThreads) void key_bounds_kernel(KeyBoundsArgs
   *(u32x4a*)(out + D) = *(const u32x4a*)hi;
 }
 
+// Blocks of a workgroup of block_score_kernel.
+template <int D>
+constexpr uint32_t kScoreBlocks = kBlockThreads / (D / 8) * 4;
+
 // Blocks of sequence b's context.
 __device__ __forceinline__ uint32_t context_blocks(const SelectArgs& a, uint32_t b, uint32_t& ctx) {
   const int32_t len = a.pg.seq[b];
@@ -158,124 +163,206 @@ __device__ __forceinline__ uint32_t score_key(float s) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// Scores of the blocks of one (sequence, KV head), a block per lane.
+// A fp64 value of lane ^ B.
+template <int B>
+__device__ __forceinline__ double lane_xor_f64(double v) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = __float_as_uint(lane_xor<B>(__uint_as_float((uint32_t)u)));
+  const uint32_t hi = __float_as_uint(lane_xor<B>(__uint_as_float((uint32_t)(u >> 32))));
+  return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
+}
+
+// Scores of the blocks of one (sequence, KV head): d / 8 lanes per block, 8 channels a lane, so that
+// a wave reads whole rows of bounds, four rounds of 4 (d = 128) or 8 blocks, all requested at the
+// start.  Four query heads at a time: their sums over the lanes meet by exchanges that halve the
+// heads a lane looks after twice, then add.
 template <int D, bool F32>
 __global__ __launch_bounds__(kBlockThreads) void block_score_kernel(SelectArgs a) {
-  constexpr uint32_t PASS = 4;                     // query heads at a time
-  extern __shared__ float s_q[];                   // [G][D]
-  const uint32_t per_row = (a.n_keys + kBlockThreads - 1) / kBlockThreads;
-  const uint32_t row = blockIdx.x / per_row, i0 = (blockIdx.x - row * per_row) * kBlockThreads;
+  constexpr uint32_t LPB = D / 8, BPW = kWave / LPB, ROUNDS = 4;
+  constexpr uint32_t PER = BPW * ROUNDS * kWavesPerBlock;              // blocks of a workgroup
+  static_assert(PER == kScoreBlocks<D>, "the host's grid");
+  const uint32_t per_row = (a.n_keys + PER - 1) / PER;
+  const uint32_t row = blockIdx.x / per_row;
   const uint32_t b = row / a.H, h = row - b * a.H;
+  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const uint32_t sub = lane % LPB;
+  const uint32_t i0 = (blockIdx.x - row * per_row) * PER + wave * BPW * ROUNDS + lane / LPB;
   uint32_t ctx;
   const uint32_t n = context_blocks(a, b, ctx);
-  if (i0 >= n) return;
-  const uint64_t q0 = (uint64_t)row * a.G * D;
-  for (uint32_t e = threadIdx.x; e < a.G * D; e += kBlockThreads) {
-    const float v = F32 ? ((const float*)a.q)[q0 + e] : widen(((const uint16_t*)a.q)[q0 + e]);
-    s_q[e] = __builtin_isfinite(v) ? v : NAN;          // both products of the sum are then NaN
+  if (i0 - lane / LPB >= n) return;
+  u32x4a lo[ROUNDS], hi[ROUNDS];
+#pragma unroll
+  for (uint32_t r = 0; r < ROUNDS; ++r) {
+    const uint32_t i = min(i0 + r * BPW, n - 1);
+    uint32_t blk = (uint32_t)a.pg.table[(size_t)b * a.pg.max_blocks + i];
+    if (blk >= a.pg.n_blocks) blk = 0;
+    const uint16_t* p = a.bounds + (((uint64_t)blk * a.H + h) * 2) * D + 8 * sub;
+    lo[r] = *(const u32x4a*)p;
+    hi[r] = *(const u32x4a*)(p + D);
   }
-  __syncthreads();
-  const uint32_t i = i0 + threadIdx.x;
-  if (i >= n) return;
-  uint32_t blk = (uint32_t)a.pg.table[(size_t)b * a.pg.max_blocks + i];
-  if (blk >= a.pg.n_blocks) blk = 0;
-  const uint16_t* lo = a.bounds + (((uint64_t)blk * a.H + h) * 2) * D;
-  uint32_t best = 0;
-  for (uint32_t g0 = 0; g0 < a.G; g0 += PASS) {
-    double acc[PASS] = {};
-    for (int c = 0; c < D; c += 8) {
-      const u32x4a vl = *(const u32x4a*)(lo + c), vh = *(const u32x4a*)(lo + D + c);
+  uint32_t best[ROUNDS] = {};
+  for (uint32_t g0 = 0; g0 < a.G; g0 += 4) {
+    double q[4][8];
+#pragma unroll
+    for (uint32_t g = 0; g < 4; ++g) {
+      const uint64_t at = ((uint64_t)row * a.G + min(g0 + g, a.G - 1)) * D + 8 * sub;
+      float x[8];
+      if constexpr (F32) {
+        const float4 u = *(const float4*)((const float*)a.q + at);
+        const float4 v = *(const float4*)((const float*)a.q + at + 4);
+        x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+      } else {
+        const u32x4a u = *(const u32x4a*)((const uint16_t*)a.q + at);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          x[k] = __uint_as_float(k % 2 ? u[k / 2] & 0xFFFF0000u : u[k / 2] << 16);
+      }
+      // not finite: NaN, which both products of the sum then are
+#pragma unroll
+      for (int k = 0; k < 8; ++k) q[g][k] = (double)__builtin_fmaf(x[k], 0.0f, x[k]);
+    }
+#pragma unroll
+    for (uint32_t r = 0; r < ROUNDS; ++r) {
+      double acc[4] = {};
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const uint32_t wl = vl[k / 2], wh = vh[k / 2];
+        const uint32_t wl = lo[r][k / 2], wh = hi[r][k / 2];
         const double x = (double)__uint_as_float(k % 2 ? wl & 0xFFFF0000u : wl << 16);
         const double y = (double)__uint_as_float(k % 2 ? wh & 0xFFFF0000u : wh << 16);
         const double mid = x + y, wide = y - x;
 #pragma unroll
-        for (uint32_t g = 0; g < PASS; ++g) {
-          const double q = (double)s_q[min(g0 + g, a.G - 1) * D + c + k];
-          acc[g] = __builtin_fma(q, mid, acc[g]);
-          acc[g] = __builtin_fma(__builtin_fabs(q), wide, acc[g]);
+        for (int g = 0; g < 4; ++g) {
+          acc[g] = __builtin_fma(q[g][k], mid, acc[g]);
+          acc[g] = __builtin_fma(__builtin_fabs(q[g][k]), wide, acc[g]);
         }
       }
+      // lanes with bit 0 of sub clear keep heads 0 and 1, then bit 1 picks one of the two
+      const bool b0 = (lane & 1) != 0, b1 = (lane & 2) != 0;
+      const double k0 = b0 ? acc[2] : acc[0], s0 = b0 ? acc[0] : acc[2];
+      const double k1 = b0 ? acc[3] : acc[1], s1 = b0 ? acc[1] : acc[3];
+      const double t0 = k0 + lane_xor_f64<1>(s0), t1 = k1 + lane_xor_f64<1>(s1);
+      double s = (b1 ? t1 : t0) + lane_xor_f64<2>(b1 ? t0 : t1);
+      s += lane_xor_f64<4>(s);
+      if constexpr (LPB == 16) s += lane_xor_f64<8>(s);
+      // the heads' scores lie on the lanes of a quad
+      uint32_t key = score_key((float)(0.5 * s));
+      key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0xB1, 0xF, 0xF, true));
+      key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0x4E, 0xF, 0xF, true));
+      best[r] = max(best[r], key);
     }
+  }
 #pragma unroll
-    for (uint32_t g = 0; g < PASS; ++g) best = max(best, score_key((float)(0.5 * acc[g])));
-  }
-  a.keys[(uint64_t)row * a.n_keys + i] = best;
+  for (uint32_t r = 0; r < ROUNDS; ++r)
+    if (sub == 0 && i0 + r * BPW < n) a.keys[(uint64_t)row * a.n_keys + i0 + r * BPW] = best[r];
 }
 
-// Exclusive prefix count of `on` over the workgroup, and the total.
-__device__ __forceinline__ uint32_t count_before(bool on, uint32_t* s_wave, uint32_t& total) {
-  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const uint64_t m = __builtin_amdgcn_ballot_w64(on);
-  if (lane == 0) s_wave[wave] = (uint32_t)__builtin_popcountll(m);
-  __syncthreads();
-  uint32_t before = __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32),
-                                              __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
-  total = 0;
-  for (uint32_t w = 0; w < kWavesPerBlock; ++w) {
-    before += w < wave ? s_wave[w] : 0u;
-    total += s_wave[w];
-  }
-  __syncthreads();
-  return before;
-}
-
-// The n_sel largest keys of one (sequence, KV head), the lower block first among equals: the
-// smallest kept key by its bytes from the top (histograms of the keys that share the bytes found so
-// far), then one pass in block order that writes the kept blocks.
-__global__ __launch_bounds__(kBlockThreads) void block_select_kernel(SelectArgs a) {
-  __shared__ uint32_t s_hist[256], s_wave[kWavesPerBlock], s_pick[2];
+// The n_sel largest keys of one (sequence, KV head), the lower block first among equals; the first
+// and last blocks stand outside the comparison.  With x = key - smallest key, the x of the last
+// kept block is found from its top down, 8 bits a step, by counting the x that share the bits found
+// so far (most steps end early: as soon as all of a bin are kept); then every thread counts the
+// kept among its KPT consecutive keys, and one scan gives their places.  KPT = 0: keys are read
+// again in every step, a thread's share of any length.
+template <int THREADS, int KPT>
+__global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
+  constexpr uint32_t WAVES = THREADS / kWave;
+  __shared__ __attribute__((aligned(16))) uint32_t s_hist[256];
+  __shared__ uint32_t s_wave[2][WAVES], s_pick[3];
   const uint32_t row = blockIdx.x, b = row / a.H, t = threadIdx.x;
+  const uint32_t lane = t % kWave, wave = t / kWave;
   uint32_t ctx;
   const uint32_t n = context_blocks(a, b, ctx);
   const uint32_t keep = min(n, a.n_sel);
-  const uint32_t* const keys = a.keys + (uint64_t)row * a.n_keys;
   int32_t* const out = a.blocks + (uint64_t)row * a.n_sel;
-  auto key = [&](uint32_t i) {
-    return i < a.n_first || i + a.n_last >= n ? 0xFFFFFFFFu : keys[i];
-  };
-  uint32_t floor_key = 0, equal = n;               // kept: key > floor_key, or the first `equal` of it
-  if (n > a.n_sel) {
-    uint32_t want = a.n_sel;                       // rank of the smallest kept key among the rest
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      s_hist[t] = 0;
-      __syncthreads();
-      const uint32_t done = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
-      for (uint32_t i = t; i < n; i += kBlockThreads) {
-        const uint32_t k = key(i);
-        if ((k & done) == (floor_key & done)) atomicAdd(&s_hist[(k >> shift) & 255u], 1u);
-      }
-      __syncthreads();
-      uint32_t above = 0;
-      for (uint32_t v = t + 1; v < 256; ++v) above += s_hist[v];
-      if (above < want && above + s_hist[t] >= want) s_pick[0] = t, s_pick[1] = above;
-      __syncthreads();
-      floor_key |= s_pick[0] << shift;
-      want -= s_pick[1];
-      __syncthreads();
-    }
-    equal = want;
-  }
-  uint32_t kept = 0, same = 0;
-  for (uint32_t i0 = 0; i0 < n; i0 += kBlockThreads) {
-    const uint32_t i = i0 + t;
-    const uint32_t k = i < n ? key(i) : 0u;
-    uint32_t more;
-    const bool eq = i < n && k == floor_key;
-    const uint32_t rank = same + count_before(eq, s_wave, more);
-    same += more;
-    const bool on = i < n && (k > floor_key || (eq && rank < equal));
-    const uint32_t at = kept + count_before(on, s_wave, more);
-    kept += more;
-    if (on && at < keep) out[at] = (int32_t)i;
-  }
-  for (uint32_t i = keep + t; i < a.n_sel; i += kBlockThreads) out[i] = -1;
   // the last block of the context is always kept, and it alone may be short
   if (t == 0)
     a.lens[row] = n == 0 ? 0 : (int32_t)(((keep - 1) << a.pg.block_log2) + ctx -
                                          ((n - 1) << a.pg.block_log2));
+  if (n <= a.n_sel) {
+    for (uint32_t i = t; i < a.n_sel; i += THREADS) out[i] = i < n ? (int32_t)i : -1;
+    return;
+  }
+  const uint32_t want = a.n_sel - a.n_first - a.n_last;              // kept between the ends
+  const uint32_t m = n - a.n_first - a.n_last;                       // blocks between them
+  for (uint32_t i = t; i < a.n_first + a.n_last; i += THREADS)
+    out[i < a.n_first ? i : want + i] = (int32_t)(i < a.n_first ? i : m + i);
+  if (want == 0) return;
+  const uint32_t* const keys = a.keys + (uint64_t)row * a.n_keys + a.n_first;
+  const uint32_t per = KPT > 0 ? (uint32_t)KPT : (m + THREADS - 1) / THREADS;
+  const uint32_t first = min(t * per, m), mine = min(per, m - first);
+  uint32_t k[KPT > 0 ? KPT : 1];
+  if constexpr (KPT > 0) {
+#pragma unroll
+    for (int c = 0; c < KPT; ++c) k[c] = keys[min(first + c, m - 1)];
+  }
+  // f(x's place, x) for each of the thread's keys
+  auto each = [&](auto&& f) {
+    if constexpr (KPT > 0) {
+#pragma unroll
+      for (int c = 0; c < KPT; ++c)
+        if ((uint32_t)c < mine) f(first + c, k[c]);
+    } else {
+      for (uint32_t c = 0; c < mine; ++c) f(first + c, keys[first + c]);
+    }
+  };
+  uint32_t low = 0xFFFFFFFFu, top = 0;
+  each([&](uint32_t, uint32_t x) { low = min(low, x), top = max(top, x); });
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) {
+    low = min(low, (uint32_t)__shfl_xor((int)low, s));
+    top = max(top, (uint32_t)__shfl_xor((int)top, s));
+  }
+  if (lane == 0) s_wave[0][wave] = low, s_wave[1][wave] = top;
+  __syncthreads();
+  for (uint32_t w = 0; w < WAVES; ++w) low = min(low, s_wave[0][w]), top = max(top, s_wave[1][w]);
+  uint32_t left = top == low ? 0u : 32u - (uint32_t)__builtin_clz(top - low);   // bits of x to find
+  uint32_t found = 0, need = want;                 // bits found; kept among those that share them
+  while (left > 0) {
+    const uint32_t w = min(left, 8u), sh = left - w;
+    __syncthreads();                               // s_wave and s_pick are read
+    for (uint32_t i = t; i < 256; i += THREADS) s_hist[i] = 0;
+    __syncthreads();
+    each([&](uint32_t, uint32_t x) {
+      const uint64_t v = x - low;
+      if ((v >> left) == found) atomicAdd(&s_hist[(uint32_t)(v >> sh) & ((1u << w) - 1u)], 1u);
+    });
+    __syncthreads();
+    if (wave == 0) {                               // lane l: bins 255 - 4 l down to 252 - 4 l
+      const uint4 v = *(const uint4*)(s_hist + 252 - 4 * lane);
+      const uint32_t sum = v.x + v.y + v.z + v.w;
+      const uint32_t end = wave_scan(sum);
+      uint32_t before = end - sum;
+      if (before < need && end >= need) {
+        const uint32_t c[4] = {v.w, v.z, v.y, v.x};
+        uint32_t i = 0;
+        while (before + c[i] < need) before += c[i++];
+        s_pick[0] = 255 - 4 * lane - i, s_pick[1] = before, s_pick[2] = c[i];
+      }
+    }
+    __syncthreads();
+    found = (found << w) | s_pick[0];
+    need -= s_pick[1];
+    left = sh;
+    if (s_pick[2] == need) break;                  // all of the bin are kept
+  }
+  // kept: x >> left above `found`, and the first `need` that equal it
+  uint32_t above = 0, equal = 0;
+  each([&](uint32_t, uint32_t x) {
+    const uint32_t v = (uint32_t)((uint64_t)(x - low) >> left);
+    above += v > found ? 1u : 0u;
+    equal += v == found ? 1u : 0u;
+  });
+  uint32_t ea = wave_scan(above), ee = wave_scan(equal);
+  __syncthreads();
+  if (lane == kWave - 1) s_wave[0][wave] = ea, s_wave[1][wave] = ee;
+  __syncthreads();
+  ea -= above, ee -= equal;
+  for (uint32_t w = 0; w < wave; ++w) ea += s_wave[0][w], ee += s_wave[1][w];
+  each([&](uint32_t i, uint32_t x) {
+    const uint32_t v = (uint32_t)((uint64_t)(x - low) >> left);
+    if (v > found || (v == found && ee < need)) out[a.n_first + ea + min(ee, need)] = (int32_t)(a.n_first + i);
+    ea += v > found ? 1u : 0u;
+    ee += v == found ? 1u : 0u;
+  });
 }
 
 template <int D, bool F32>
@@ -293,8 +380,18 @@ void launch_bounds(const KeyBoundsArgs& a, hipStream_t s) {
 
 template <int D, bool F32>
 void launch_scores(const SelectArgs& a, hipStream_t s) {
-  const uint32_t per_row = (a.n_keys + kBlockThreads - 1) / kBlockThreads;
-  hipLaunchKernelGGL((block_score_kernel<D, F32>), dim3(per_row * a.B * a.H), dim3(kBlockThreads), a.G * D * 4, s, a);
+  const uint32_t per_row = (a.n_keys + kScoreBlocks<D> - 1) / kScoreBlocks<D>;
+  hipLaunchKernelGGL((block_score_kernel<D, F32>), dim3(per_row * a.B * a.H), dim3(kBlockThreads), 0, s, a);
+}
+
+void launch_select(const SelectArgs& a, hipStream_t s) {
+  const dim3 grid(a.B * a.H);
+  if (a.n_keys <= 256 * 4)
+    hipLaunchKernelGGL((block_select_kernel<256, 4>), grid, dim3(256), 0, s, a);
+  else if (a.n_keys <= 1024 * 16)
+    hipLaunchKernelGGL((block_select_kernel<1024, 16>), grid, dim3(1024), 0, s, a);
+  else
+    hipLaunchKernelGGL((block_select_kernel<1024, 0>), grid, dim3(1024), 0, s, a);
 }
 
 }  // namespace
@@ -314,6 +411,6 @@ int tvq_launch_select(const tvq::SelectArgs& a, int d, bool f32, void* stream) {
   else if (d == 64) f32 ? tvq::launch_scores<64, true>(a, s) : tvq::launch_scores<64, false>(a, s);
   else return -1;
   if (hipGetLastError() != hipSuccess) return -2;
-  hipLaunchKernelGGL(tvq::block_select_kernel, dim3(a.B * a.H), dim3(tvq::kBlockThreads), 0, s, a);
+  tvq::launch_select(a, s);
   return hipGetLastError() == hipSuccess ? 0 : -2;
 }
