@@ -70,9 +70,12 @@ struct RowsPlan {
 // context; d: head dimension; cus: compute units.
 //
 // Up to 32 rows a wave works by itself, with its own tile in LDS; above, four waves share a tile.
-// The spans of a launch fill the places that the device has for its workgroups (8 single waves or 2
-// workgroups of four a compute unit), of at least 128 or 256 tokens each, so that a span's start
-// and its partial stay small beside it.
+// The spans of a launch go to the places that the device has for its workgroups (8 single waves or
+// 2 workgroups of four a compute unit), so many at a time; a span costs its tiles and, for its start
+// and its partial, about kSpanTiles more.  The number of spans with the least time for full
+// contexts is taken, of at least 128 or 256 tokens each.
+constexpr int64_t kSpanTiles = 3;
+
 inline RowsPlan rows_plan(int64_t batch, int64_t heads, int64_t rows, int64_t tokens, int32_t d,
                           int64_t cus) {
   const auto ceil_div = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
@@ -85,10 +88,16 @@ inline RowsPlan rows_plan(int64_t batch, int64_t heads, int64_t rows, int64_t to
   p.n_rb = (uint32_t)n_rb;
   p.units = batch * heads * n_rb;
   const int64_t places = cus * (p.waves == 1 ? 8 : 2);
-  int64_t n = ceil_div(places, p.units);
+  const int64_t tiles = ceil_div(tokens, p.tile);
+  const int64_t fill = 4 * places / p.units + 1;      // past four rounds of places nothing is gained
   const int64_t most = tokens / (p.min_tiles * (int64_t)p.tile);
-  n = n < most ? n : most;
-  p.n_split = (uint32_t)(n < 1 ? 1 : n);
+  const auto time = [&](int64_t n) {
+    return ceil_div(p.units * n, places) * (ceil_div(tiles, n) + (n > 1 ? kSpanTiles : 0));
+  };
+  int64_t best = 1;
+  for (int64_t n = 2; n <= most && n <= fill; ++n)
+    if (time(n) < time(best)) best = n;
+  p.n_split = (uint32_t)best;
   const int64_t parts = p.n_split > 1 ? p.units * p.n_split * p.unit_rows : 0;
   p.acc_bytes = (parts * d * 4 + 255) / 256 * 256;
   p.ws_bytes = p.acc_bytes + parts * 8;

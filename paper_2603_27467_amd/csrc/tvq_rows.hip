@@ -644,10 +644,12 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 1 ? 2 : 2) void rows_kernel
 }
 
 // The spans of one row, a row per wave, its elements across the lanes: M = max m, then
-// o = D W (sum 2^(m - M) acc) / (sum 2^(m - M) l).
+// o = D W (sum 2^(m - M) acc) / (sum 2^(m - M) l).  The spans' (m, l) are read 64 at a time, one
+// per lane, and 8 spans' rows are requested together, the first ones before M is known.
 template <int D>
 __global__ __launch_bounds__(kBlockThreads) void rows_merge_kernel(RowsArgs a) {
   constexpr int EPL = D / kWave;
+  constexpr uint32_t kRows = 8;
   const int lane = threadIdx.x & (kWave - 1);
   const uint32_t i = __builtin_amdgcn_readfirstlane(blockIdx.x * kWavesPerBlock + threadIdx.x / kWave);
   const uint32_t unit = i / a.unit_rows, in_unit = i - unit * a.unit_rows;
@@ -657,23 +659,49 @@ __global__ __launch_bounds__(kBlockThreads) void rows_merge_kernel(RowsArgs a) {
   if (row >= u.rows) return;
   const uint32_t spans = row_spans((u.tokens + a.tile - 1) / a.tile, a.n_split, a.min_tiles);
   const uint64_t part = (uint64_t)unit * a.n_split * a.unit_rows + in_unit;
-  float M = kNoScore;
-  for (uint32_t s = 0; s < spans; ++s) M = fmaxf(M, a.ws_ml[(part + (uint64_t)s * a.unit_rows) * 2]);
+  const float* const ml = a.ws_ml + part * 2;
+  const float* const acc = a.ws_acc + part * D + EPL * lane;
+  const size_t next = (size_t)a.unit_rows;              // partials of the next span
+  auto load_ml = [&](uint32_t s) {
+    return s < spans ? *(const float2*)(ml + s * next * 2) : make_float2(kNoScore, 0.0f);
+  };
+  float r[kRows][EPL];
+  auto load_acc = [&](uint32_t s0) {
+#pragma unroll
+    for (uint32_t k = 0; k < kRows; ++k)
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) r[k][e] = acc[min(s0 + k, spans - 1) * next * D + e];
+  };
+  float2 v = load_ml(lane);
+  load_acc(0);
+  const uint32_t smw = a.signs[(EPL * lane) / 2];
+  float M = v.x;
+  for (uint32_t s = (uint32_t)lane + kWave; s < spans; s += kWave) M = fmaxf(M, load_ml(s).x);
+  M = wave_max(M);
   float L = 0.0f, x[EPL];
 #pragma unroll
   for (int e = 0; e < EPL; ++e) x[e] = 0.0f;
-  for (uint32_t s = 0; s < spans; ++s) {
-    const uint64_t p = part + (uint64_t)s * a.unit_rows;
-    const float f = __builtin_amdgcn_exp2f(a.ws_ml[p * 2] - M);
-    L = __builtin_fmaf(a.ws_ml[p * 2 + 1], f, L);
+  for (uint32_t s0 = 0; s0 < spans; s0 += kWave) {
+    if (s0 != 0) v = load_ml(s0 + lane);
+    const float w = __builtin_amdgcn_exp2f(v.x - M);
+    L = __builtin_fmaf(v.y, w, L);
+    const uint32_t n = min(spans - s0, (uint32_t)kWave);
+    for (uint32_t k0 = 0; k0 < n; k0 += kRows) {
+      if (s0 + k0 != 0) load_acc(s0 + k0);
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) x[e] = __builtin_fmaf(a.ws_acc[p * D + EPL * lane + e], f, x[e]);
+      for (uint32_t k = 0; k < kRows; ++k) {
+        const float f = s0 + k0 + k < spans ? lane_value(w, (int)(k0 + k)) : 0.0f;
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) x[e] = __builtin_fmaf(r[k][e], f, x[e]);
+      }
+    }
   }
+  L = wave_sum(L);
   const float inv = 1.0f / L;
 #pragma unroll
   for (int e = 0; e < EPL; ++e) x[e] = M == kNoScore ? 0.0f : x[e] * inv;
   fwht_across_lanes<EPL>(x, lane);
-  apply_signs<EPL>(x, a.signs[(EPL * lane) / 2], lane);
+  apply_signs<EPL>(x, smw, lane);
   const uint32_t j = row / a.G, g = row - j * a.G;
   const uint64_t at = (uint64_t)u.b * a.o_stride[0] + (uint64_t)(u.h * a.G + g) * a.o_stride[1] +
                       (uint64_t)j * a.o_stride[2] + EPL * lane;
