@@ -61,7 +61,7 @@ TVQ_ROWS_HOST_DEVICE uint32_t span_start(uint32_t tiles, uint32_t n, uint32_t k)
 }
 
 struct RowsPlan {
-  uint32_t waves;        // of a workgroup: 1 or 4
+  uint32_t waves;        // of a workgroup: 1, 4 or 8
   uint32_t unit_rows, tile, n_rb, n_split, min_tiles;
   int64_t units, acc_bytes, ws_bytes;
 };
@@ -80,14 +80,14 @@ inline RowsPlan rows_plan(int64_t batch, int64_t heads, int64_t rows, int64_t to
                           int64_t cus) {
   const auto ceil_div = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
   RowsPlan p;
-  p.waves = rows <= 32 ? 1 : 4;
+  p.waves = rows <= 32 ? 1 : rows <= 128 ? 4 : 8;
   p.unit_rows = p.waves * 32;
   p.tile = p.waves == 1 ? 32 : 64;
   p.min_tiles = 4;
   const int64_t n_rb = ceil_div(rows, p.unit_rows);
   p.n_rb = (uint32_t)n_rb;
   p.units = batch * heads * n_rb;
-  const int64_t places = cus * (p.waves == 1 ? 8 : 2);
+  const int64_t places = cus * (p.waves == 1 ? 8 : p.waves == 4 ? 2 : 1);
   const int64_t tiles = ceil_div(tokens, p.tile);
   const int64_t fill = 4 * places / p.units + 1;      // past four rounds of places nothing is gained
   const int64_t most = tokens / (p.min_tiles * (int64_t)p.tile);

@@ -43,6 +43,8 @@
 #include <float.h>
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "tvq_codes.h"
 #include "tvq_device.h"
 #include "tvq_internal.h"
@@ -124,7 +126,7 @@ struct Shape {
   static constexpr int CHUNKS = D / 8;
   static constexpr int PLANE = TILE * ROW;
   static constexpr int KIND = PARTS * PLANE;
-  static constexpr int BUFS = WAVES == 1 || PARTS == 2 ? 1 : 2;
+  static constexpr int BUFS = WAVES == 1 || (WAVES == 4 && PARTS == 2) ? 1 : 2;
   static constexpr int LUT = 256 * 4 * PARTS;
 };
 
@@ -205,9 +207,15 @@ __device__ __forceinline__ int rebuild(const RawCodes& raw, uint32_t n, bool log
     const float l0 = __builtin_amdgcn_logf(lo == hi ? rmin : lo);
     const float step = lo == hi ? 0.0f : (__builtin_amdgcn_logf(hi) - l0) * (1.0f / 15.0f);
     const float base = l0 - (float)e;
+    uint32_t nib[4];                             // code 8 j + 2 k + s: byte k of nib[2 j + s]
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      nib[2 * j] = raw.nrm[j] & 0x0F0F0F0Fu;
+      nib[2 * j + 1] = (raw.nrm[j] >> 4) & 0x0F0F0F0Fu;
+    }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float q = (float)((raw.nrm[i / 8] >> (4 * (i % 8))) & 15u);
+      const float q = (float)((nib[2 * (i / 8) + i % 2] >> (8 * (i % 8 / 2))) & 255u);
       r[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(q, step, base));
     }
   } else {
@@ -224,8 +232,8 @@ __device__ __forceinline__ int rebuild(const RawCodes& raw, uint32_t n, bool log
       const int i = 4 * j + k;
       if constexpr (PARTS == 1) {
         const h2 cs = ((const h2*)lut)[c[i]];
-        const h2 rr = cvt_h2(r[i], r[i]);
-        hi[k] = h2_bits(rr * cs);
+        const h2 rr = cvt_h2(r[i & ~1], r[i | 1]);
+        hi[k] = h2_bits((i % 2 ? (h2){rr.y, rr.y} : (h2){rr.x, rr.x}) * cs);
       } else {
         const float2 cs = ((const float2*)lut)[c[i]];
         const float x = r[i] * cs.x, y = r[i] * cs.y;
@@ -435,7 +443,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 1 ? 2 : 2) void rows_kernel
   };
   const uint32_t sub = (uint32_t)lane % S::LPV, vec = (uint32_t)lane / S::LPV;
   RawCodes raw[S::TASKS];
-  auto load_tile = [&](uint32_t tile) {
+  auto load_tile = [&](uint32_t tile) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < S::TASKS; ++k) {
       const uint32_t task = wave + WAVES * k;
@@ -455,7 +463,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 1 ? 2 : 2) void rows_kernel
       raw[k] = load_raw(a, kind, D, slot0, jj, sub);
     }
   };
-  auto rebuild_tile = [&](int buf) {
+  auto rebuild_tile = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < S::TASKS; ++k) {
       const uint32_t task = wave + WAVES * k;
@@ -475,115 +483,126 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 1 ? 2 : 2) void rows_kernel
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) acc[i] = (v16f)(0.0f);
 
-  auto work = [&](int buf, uint32_t tile) {
-#pragma unroll 1
-    for (int part = 0; part < S::TILE / 32; ++part) {
-      const uint32_t tb = tile * S::TILE + 32 * part;
-      if (tb >= lim_hi) break;
-      // ---- scores ----
-      const char* const kt = s_tile[buf][0] + (32 * part + (lane & 31)) * S::ROW;
-      v16f s = (v16f)(0.0f);
+  // the lane's places in a tile of keys (its token's row, by k) and of values (by element block and
+  // half of the 16 tokens)
+  uint32_t ka[D / 16], va[D / 32][2];
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        const uint32_t at = 16u * key_chunk<D>(2 * k + half, lane & 31);
-        const h8 kh = read_h8(kt + at);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh, q[0][k], s, 0, 0, 0);
-        if constexpr (PARTS == 2) {
-          const h8 kl = read_h8(kt + at + S::PLANE);
-          s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh, q[1][k], s, 0, 0, 0);
-          s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kl, q[0][k], s, 0, 0, 0);
-        }
+  for (int k = 0; k < D / 16; ++k)
+    ka[k] = (lane & 31) * S::ROW + 16u * key_chunk<D>(2 * k + half, lane & 31);
+#pragma unroll
+  for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const uint32_t tk = 8 * z + 4 * half + (((uint32_t)lane >> 2) & 3u);
+      const uint32_t chunk = 4 * mb + 2 * (((uint32_t)lane >> 4) & 1u) + (((uint32_t)lane >> 1) & 1u);
+      va[mb][z] = tk * S::ROW + 16u * (chunk ^ value_swap<D>(tk)) + 8u * (lane & 1);
+    }
+
+  // 32 tokens from `tb` on, at offset `part` of the tile in `buf`
+  auto work32 = [&](auto buf_c, auto part_c, uint32_t tb) __attribute__((always_inline)) {
+    constexpr int buf = decltype(buf_c)::value, part = decltype(part_c)::value;
+    // ---- scores ----
+    const char* const kt = s_tile[buf][0] + 32 * part * S::ROW;
+    v16f s = (v16f)(0.0f);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      const h8 kh = read_h8(kt + ka[k]);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh, q[0][k], s, 0, 0, 0);
+      if constexpr (PARTS == 2) {
+        const h8 kl = read_h8(kt + ka[k] + S::PLANE);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh, q[1][k], s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kl, q[0][k], s, 0, 0, 0);
       }
-      // registers 0 .. 7 hold the tokens of the first group of 16, 8 .. 15 those of the second
-      float x[16];
-      int ve[2];
+    }
+    // registers 0 .. 7 hold the tokens of the first group of 16, 8 .. 15 those of the second
+    if (tb + 32 > lim_lo) {
+      const uint32_t t = tb + 4 * half;
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int group = (32 * part + 16 * p) / S::GROUP;
-        const float f = fmaxf(qf * pow2i(__builtin_amdgcn_readfirstlane(s_exp[buf][0][group])), FLT_MIN);
-        ve[p] = __builtin_amdgcn_readfirstlane(s_exp[buf][1][group]);
+      for (int i = 0; i < 16; ++i) s[i] = t + (i % 4) + 8 * (i / 4) < lim ? s[i] : -INFINITY;
+    }
+    float f[2], top = -INFINITY;
+    int ve[2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[8 * p + i] = s[8 * p + i] * f;
-      }
-      if (tb + 32 > lim_lo) {
+    for (int p = 0; p < 2; ++p) {
+      const int group = (32 * part + 16 * p) / S::GROUP;
+      f[p] = fmaxf(qf * pow2i(__builtin_amdgcn_readfirstlane(s_exp[buf][0][group])), FLT_MIN);
+      ve[p] = __builtin_amdgcn_readfirstlane(s_exp[buf][1][group]);
+      float mx = s[8 * p];
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          x[i] = tb + (i % 4) + 8 * (i / 4) + 4 * half < lim ? x[i] : -INFINITY;
-      }
-      float top = x[0];
+      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[8 * p + i]);
+      top = fmaxf(top, mx * f[p]);
+    }
+    if (__builtin_amdgcn_ballot_w64(top > m + (kLazy + kBias)) != 0) {
+      float lo, hi;
+      halves(top, lo, hi);
+      // rows that stay below keep their reference: a row's bits do not depend on its neighbours
+      const float most = fmaxf(lo, hi);
+      const float mn = most > m + (kLazy + kBias) ? most - kBias : m;
+      const float down = __builtin_amdgcn_exp2f(m - mn);
+      l *= down;
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-      if (__builtin_amdgcn_ballot_w64(top > m + (kLazy + kBias)) != 0) {
-        float lo, hi;
-        halves(top, lo, hi);
-        // rows that stay below keep their reference: a row's bits do not depend on its neighbours
-        const float most = fmaxf(lo, hi);
-        const float mn = most > m + (kLazy + kBias) ? most - kBias : m;
-        const float f = __builtin_amdgcn_exp2f(m - mn);
-        l *= f;
+      for (int i = 0; i < D / 32; ++i) acc[i] *= down;
+      m = mn;
+    }
+    const int vmax = max(ve[0], ve[1]);
+    if (vmax > vexp) {
+      const float down = pow2i(vexp - vmax);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) acc[i] *= f;
-        m = mn;
-      }
-      // ---- weights ----
-      const int vmax = max(ve[0], ve[1]);
-      if (vmax > vexp) {
-        const float f = pow2i(vexp - vmax);
+      for (int i = 0; i < D / 32; ++i) acc[i] *= down;
+      vexp = vmax;
+    }
+    // ---- weights (their sum is that of the rounded ones) and values, 16 tokens at a time ----
+    const char* const vt = s_tile[buf][1] + 32 * part * S::ROW;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) acc[i] *= f;
-        vexp = vmax;
-      }
-      float w[16];
+    for (int p = 0; p < 2; ++p) {
+      h8 ph, pl;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        w[i] = __builtin_amdgcn_exp2f(x[i] - m);
-        l += w[i];
-      }
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-        if (ve[p] != vexp) {
-          const float f = pow2i(ve[p] - vexp);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) w[8 * p + i] *= f;
-        }
-      // ---- values: 16 tokens at a time ----
-      const uint32_t quad = ((uint32_t)lane >> 2) & 3u;      // row of the transposing read
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        h8 ph, pl;
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-          const h2 v = cvt_h2(w[8 * p + i], w[8 * p + i + 1]);
+      for (int i = 0; i < 8; i += 2) {
+        float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * p + i], f[p], -m));
+        float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * p + i + 1], f[p], -m));
+        if constexpr (PARTS == 1) {
+          const h2 v = cvt_h2(w0, w1);
+          l = __builtin_amdgcn_fdot2(v, (h2){(_Float16)1.0f, (_Float16)1.0f}, l, false);
           ph[i] = v.x, ph[i + 1] = v.y;
+        } else {
+          l += w0 + w1;
+          if (ve[p] != vexp) {
+            const float down = pow2i(ve[p] - vexp);
+            w0 *= down, w1 *= down;
+          }
+          const h2 v = cvt_h2(w0, w1), z = cvt_h2(w0 - (float)v.x, w1 - (float)v.y);
+          ph[i] = v.x, ph[i + 1] = v.y;
+          pl[i] = z.x, pl[i + 1] = z.y;
+        }
+      }
+      if constexpr (PARTS == 1)
+        if (ve[p] != vexp) ph *= (_Float16)pow2i(ve[p] - vexp);
+#pragma unroll
+      for (int mb = 0; mb < D / 32; ++mb) {
+        h8 vh, vl;
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const char* const at = vt + va[mb][z] + 16 * p * S::ROW;
+          const s4 c = read_columns(at);
+          __builtin_memcpy((char*)&vh + 8 * z, &c, 8);
           if constexpr (PARTS == 2) {
-            const h2 z = cvt_h2(w[8 * p + i] - (float)v.x, w[8 * p + i + 1] - (float)v.y);
-            pl[i] = z.x, pl[i + 1] = z.y;
+            const s4 cl = read_columns(at + S::PLANE);
+            __builtin_memcpy((char*)&vl + 8 * z, &cl, 8);
           }
         }
-#pragma unroll
-        for (int mb = 0; mb < D / 32; ++mb) {
-          h8 vh, vl;
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const uint32_t t = 16 * p + 8 * z + 4 * half + quad;
-            const uint32_t chunk = 4 * mb + 2 * (((uint32_t)lane >> 4) & 1u) + (((uint32_t)lane >> 1) & 1u);
-            const char* const at = s_tile[buf][1] + (32 * part + t) * S::ROW +
-                                   16u * (chunk ^ value_swap<D>(t)) + 8u * (lane & 1);
-            const s4 c = read_columns(at);
-            __builtin_memcpy((char*)&vh + 8 * z, &c, 8);
-            if constexpr (PARTS == 2) {
-              const s4 cl = read_columns(at + S::PLANE);
-              __builtin_memcpy((char*)&vl + 8 * z, &cl, 8);
-            }
-          }
-          acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, ph, acc[mb], 0, 0, 0);
-          if constexpr (PARTS == 2) {
-            acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, pl, acc[mb], 0, 0, 0);
-            acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vl, ph, acc[mb], 0, 0, 0);
-          }
+        acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, ph, acc[mb], 0, 0, 0);
+        if constexpr (PARTS == 2) {
+          acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, pl, acc[mb], 0, 0, 0);
+          acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vl, ph, acc[mb], 0, 0, 0);
         }
       }
     }
+  };
+  auto work = [&](auto buf_c, uint32_t tile) __attribute__((always_inline)) {
+    const uint32_t tb = tile * S::TILE;
+    if (busy && tb < lim_hi) work32(buf_c, std::integral_constant<int, 0>{}, tb);
+    if constexpr (S::TILE > 32)
+      if (busy && tb + 32 < lim_hi) work32(buf_c, std::integral_constant<int, 1>{}, tb + 32);
   };
 
   if (t0 < t1) {
@@ -596,19 +615,23 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 1 ? 2 : 2) void rows_kernel
       rebuild_tile(0);
       if (t + 1 < t1) load_tile(t + 1);
       __syncthreads();
-      if (busy) work(0, t);
+      work(std::integral_constant<int, 0>{}, t);
     }
   } else {
+    // two tiles a round, so that the places in LDS are known when it is compiled
+    auto step = [&](auto buf_c, uint32_t t) __attribute__((always_inline)) {
+      if (t + 1 < t1) rebuild_tile(decltype(buf_c)::value ^ 1);
+      if (t + 2 < t1) load_tile(t + 2);
+      work(buf_c, t);
+      __syncthreads();
+    };
     __syncthreads();
     if (t0 < t1) rebuild_tile(0);
     if (t0 + 1 < t1) load_tile(t0 + 1);
     __syncthreads();
-    for (uint32_t t = t0; t < t1; ++t) {
-      const int buf = (int)((t - t0) & 1u);
-      if (t + 1 < t1) rebuild_tile(buf ^ 1);
-      if (t + 2 < t1) load_tile(t + 2);
-      if (busy) work(buf, t);
-      __syncthreads();
+    for (uint32_t t = t0; t < t1; t += 2) {
+      step(std::integral_constant<int, 0>{}, t);
+      if (t + 1 < t1) step(std::integral_constant<int, 1>{}, t + 1);
     }
   }
   if (!busy) return;
@@ -721,6 +744,9 @@ int launch(const RowsArgs& a, unsigned waves, bool wide, hipStream_t s) {
   if (waves == 1) {
     if (wide) hipLaunchKernelGGL((rows_kernel<D, 1, 2>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((rows_kernel<D, 1, 1>), grid, block, 0, s, a);
+  } else if (waves == 8) {
+    if (wide) hipLaunchKernelGGL((rows_kernel<D, 8, 2>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((rows_kernel<D, 8, 1>), grid, block, 0, s, a);
   } else {
     if (wide) hipLaunchKernelGGL((rows_kernel<D, 4, 2>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((rows_kernel<D, 4, 1>), grid, block, 0, s, a);
