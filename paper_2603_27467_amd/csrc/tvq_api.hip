@@ -1091,7 +1091,12 @@ static tvq_status rows_launch(const tvq_codec* c, tvq::RowsArgs& a, const void* 
   a.o = o;
   for (int k = 0; k < 3; ++k) a.q_stride[k] = q_stride[k], a.o_stride[k] = o_stride[k];
   a.ws_acc = (float*)workspace;
-  a.ws_ml = p.ws_bytes > 0 ? (float*)((char*)workspace + p.acc_bytes) : nullptr;
+  a.ws_ml = (float*)((char*)workspace + p.acc_bytes);
+  if (p.tile_bytes > 0 && o_dtype == TVQ_BF16) {
+    a.n_tiles = (uint32_t)p.n_tiles;
+    a.ws_tiles = (char*)workspace + p.acc_bytes + p.ml_bytes;
+    a.ws_exps = (int*)(a.ws_tiles + p.tile_bytes);
+  }
   const int rc = tvq_launch_rows(a, c->d, p.waves, o_dtype == TVQ_F32, stream);
   if (rc == -1) return TVQ_ERR_UNSUPPORTED;
   return rc == 0 ? TVQ_OK : TVQ_ERR_HIP;

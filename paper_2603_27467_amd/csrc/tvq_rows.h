@@ -45,6 +45,9 @@ struct RowsArgs {
   const uint8_t* plane[2][3];
   float* ws_acc;         // [unit][span][unit_rows][d]
   float* ws_ml;          // [unit][span][unit_rows][2]
+  uint32_t n_tiles;      // tiles of a context of t_end
+  char* ws_tiles;        // rebuilt tiles [B][H][n_tiles][keys, values] (nullptr: every workgroup
+  int* ws_exps;          // rebuilds its own), and their exponents
 };
 
 // Spans that a unit of `tiles` tiles is cut into.
@@ -63,8 +66,15 @@ TVQ_ROWS_HOST_DEVICE uint32_t span_start(uint32_t tiles, uint32_t n, uint32_t k)
 struct RowsPlan {
   uint32_t waves;        // of a workgroup: 1, 4 or 8
   uint32_t unit_rows, tile, n_rb, n_split, min_tiles;
-  int64_t units, acc_bytes, ws_bytes;
+  int64_t units, acc_bytes, ml_bytes;
+  int64_t n_tiles, tile_bytes, exp_bytes;   // rebuilt tiles (0: none)
+  int64_t ws_bytes;
 };
+
+// Rebuilding the tiles of all tokens once costs a launch and 4 d bytes a token and head written and
+// read back; every unit but one of a (sequence, KV head) is spared it.
+constexpr int64_t kRebuildUnits = 4;                 // units from which on the tiles are kept
+constexpr int64_t kRebuildBytes = 1ll << 31;         // and the most they may take
 
 // batch, heads: of the cache; rows: query rows of a (sequence, KV head); tokens: bound of a
 // context; d: head dimension; cus: compute units.
@@ -100,7 +110,13 @@ inline RowsPlan rows_plan(int64_t batch, int64_t heads, int64_t rows, int64_t to
   p.n_split = (uint32_t)best;
   const int64_t parts = p.n_split > 1 ? p.units * p.n_split * p.unit_rows : 0;
   p.acc_bytes = (parts * d * 4 + 255) / 256 * 256;
-  p.ws_bytes = p.acc_bytes + parts * 8;
+  p.ml_bytes = (parts * 8 + 255) / 256 * 256;
+  p.n_tiles = tiles;
+  p.tile_bytes = batch * heads * tiles * p.tile * 4 * d;
+  p.exp_bytes = batch * heads * tiles * 32;           // at most 8 groups of 4 bytes
+  if (p.waves < 8 || n_rb < kRebuildUnits || p.tile_bytes > kRebuildBytes)
+    p.n_tiles = p.tile_bytes = p.exp_bytes = 0;
+  p.ws_bytes = p.acc_bytes + p.ml_bytes + p.tile_bytes + p.exp_bytes;
   return p;
 }
 

@@ -126,7 +126,6 @@ struct Shape {
   static constexpr int CHUNKS = D / 8;
   static constexpr int PLANE = TILE * ROW;
   static constexpr int KIND = PARTS * PLANE;
-  static constexpr int BUFS = WAVES == 1 || (WAVES == 4 && PARTS == 2) ? 1 : 2;
   static constexpr int LUT = 256 * 4 * PARTS;
 };
 
@@ -381,55 +380,204 @@ __device__ __forceinline__ float load_rows(const RowsArgs& a, uint64_t at, int h
   return pow2i(e);
 }
 
-template <int D, int WAVES, int PARTS>
-__global__ __launch_bounds__(WAVES * kWave, WAVES == 1 ? 2 : 2) void rows_kernel(RowsArgs a) {
-  using S = Shape<D, WAVES, PARTS>;
-  __shared__ __attribute__((aligned(16))) char s_lut[2][S::LUT];
-  __shared__ __attribute__((aligned(16))) char s_tile[S::BUFS][2][S::KIND];
-  __shared__ int s_exp[S::BUFS][2][S::NG];
-  const uint32_t wave = WAVES == 1 ? 0u : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int lane = threadIdx.x % kWave, half = lane >> 5;
-  // units with the most tokens first (the last rows see the most), a unit's spans together; the
-  // (sequence, KV head) goes round the XCDs, so that its units meet in one L2
-  const uint32_t heads = a.B * a.H;
-  const uint32_t bh = blockIdx.x % heads, rest = blockIdx.x / heads;
-  const uint32_t span = rest % a.n_split, rb = a.n_rb - 1 - rest / a.n_split;
-  const uint32_t unit = rb * heads + bh;
-  const Unit u = unit_at(a, unit);
-  const uint32_t row0 = rb * (WAVES * 32);
-  if (row0 >= u.rows) return;
-  const uint32_t tiles = (u.tokens + S::TILE - 1) / S::TILE;
-  const uint32_t spans = row_spans(tiles, a.n_split, a.min_tiles);
-  if (span >= spans) return;
-  const uint32_t t0 = span_start(tiles, spans, span), t1 = span_start(tiles, spans, span + 1);
+// What the 32 tokens' groups of 16 are scaled by: exponents of the keys and of the values.
+struct Scales {
+  int ke[2], ve[2];
+};
 
-  // tables
-  for (int kind = 0; kind < 2; ++kind)
-    for (uint32_t i = threadIdx.x; i < a.n[kind]; i += WAVES * kWave) {
-      const float2 cs = ((const float2*)a.lut[kind])[i];
-      if constexpr (PARTS == 1) ((h2*)s_lut[kind])[i] = cvt_h2(cs.x, cs.y);
-      else ((float2*)s_lut[kind])[i] = cs;
-    }
-
-  // the lane's query row (past the last: the last, not stored)
-  const uint32_t row = row0 + wave * 32 + (lane & 31);
-  const bool on = row < u.rows;
-  const bool busy = row0 + wave * 32 < u.rows;          // the wave has rows
-  const uint32_t r = min(row, u.rows - 1);
-  const uint32_t j = r / a.G, g = r - j * a.G;
-  const uint64_t q_at = (uint64_t)u.b * a.q_stride[0] + (uint64_t)(u.h * a.G + g) * a.q_stride[1] +
-                        (uint64_t)j * a.q_stride[2];
+// 32 query rows, one on each pair of lanes l and l + 32: queries, statistics, accumulators, and the
+// steps of the softmax.
+template <int D, int PARTS>
+struct Rows {
+  uint32_t j, g;                                // token and query head of the lane's row
+  uint32_t in_unit;                             // its place in the unit
+  bool on, busy;                                // the row, and any of the 32, is one
+  uint32_t lim, lim_lo, lim_hi;                 // tokens that the row sees; fewest and most of the 32
   h8 q[PARTS][D / 16];
-  const float qf = load_rows<D, PARTS>(a, q_at, half, q);
-  const int64_t seen = u.pos0 + j + 1;                   // tokens that the row sees
-  const uint32_t lim = seen < 0 ? 0u : (uint32_t)seen;
-  // the least and the most of the wave's rows: its first and its last
-  const uint32_t lim_lo = (uint32_t)__builtin_amdgcn_readlane((int)lim, 0);
-  const uint32_t lim_hi = (uint32_t)__builtin_amdgcn_readlane((int)lim, 31);
+  float qf;
+  float m, l;
+  int vexp;                                     // E of the accumulators
+  v16f acc[D / 32];
 
-  // pool blocks: lane i holds that of the sequence's (or the list's) block blk0 + i
-  uint32_t blk0 = 0, blk = 0;
-  auto load_blocks = [&](uint32_t first) {
+  // Rows from `first` of the unit on (past the sequence's last: that one, not stored).
+  __device__ __forceinline__ void start(const RowsArgs& a, const Unit& u, uint32_t first, int lane) {
+    const uint32_t row0 = u.rb * a.unit_rows + first;
+    in_unit = first + (lane & 31);
+    on = row0 + (lane & 31) < u.rows;
+    busy = row0 < u.rows;
+    const uint32_t r = min(row0 + (lane & 31), u.rows - 1);
+    j = r / a.G;
+    g = r - j * a.G;
+    const int64_t seen = u.pos0 + j + 1;
+    lim = seen < 0 ? 0u : (uint32_t)seen;
+    lim_lo = (uint32_t)__builtin_amdgcn_readlane((int)lim, 0);     // rows in order of their tokens
+    lim_hi = (uint32_t)__builtin_amdgcn_readlane((int)lim, 31);
+    const uint64_t at = (uint64_t)u.b * a.q_stride[0] + (uint64_t)(u.h * a.G + g) * a.q_stride[1] +
+                        (uint64_t)j * a.q_stride[2];
+    qf = load_rows<D, PARTS>(a, at, lane >> 5, q);
+    m = kNoScore;
+    l = 0.0f;
+    vexp = kNoExp;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) acc[i] = (v16f)(0.0f);
+  }
+
+  __device__ __forceinline__ float factor(const Scales& c, int p) const {
+    return fmaxf(qf * pow2i(c.ke[p]), FLT_MIN);
+  }
+
+  __device__ __forceinline__ void lower(float by) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) acc[i] *= by;
+  }
+
+  // Before the weights of 32 tokens from tb on: scores that a row does not see, the reference point,
+  // the accumulators' exponent.  Registers 0 .. 7 of s hold the first 16 tokens, 8 .. 15 the second.
+  __device__ __forceinline__ void settle(v16f& s, const Scales& c, uint32_t tb, int half) {
+    if (tb + 32 > lim_lo) {
+      const uint32_t t = tb + 4 * half;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = t + (i % 4) + 8 * (i / 4) < lim ? s[i] : -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      float mx = s[8 * p];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[8 * p + i]);
+      top = fmaxf(top, mx * factor(c, p));
+    }
+    if (__builtin_amdgcn_ballot_w64(top > m + (kLazy + kBias)) != 0) {
+      float lo, hi;
+      halves(top, lo, hi);
+      // rows that stay below keep their reference: a row's bits do not depend on its neighbours
+      const float most = fmaxf(lo, hi);
+      const float mn = most > m + (kLazy + kBias) ? most - kBias : m;
+      const float down = __builtin_amdgcn_exp2f(m - mn);
+      l *= down;
+      lower(down);
+      m = mn;
+    }
+    const int vmax = max(c.ve[0], c.ve[1]);
+    if (vmax > vexp) {
+      lower(pow2i(vexp - vmax));
+      vexp = vmax;
+    }
+  }
+
+  // The weights as operands; bf16 outputs take the sum of the rounded ones.
+  __device__ __forceinline__ void weigh(const v16f& s, const Scales& c, h8 (&w)[PARTS][2]) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const float f = factor(c, p);
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * p + i], f, -m));
+        float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * p + i + 1], f, -m));
+        if constexpr (PARTS == 1) {
+          const h2 v = cvt_h2(w0, w1);
+          l = __builtin_amdgcn_fdot2(v, (h2){(_Float16)1.0f, (_Float16)1.0f}, l, false);
+          w[0][p][i] = v.x, w[0][p][i + 1] = v.y;
+        } else {
+          l += w0 + w1;
+          const float down = pow2i(c.ve[p] - vexp);
+          w0 *= down, w1 *= down;
+          const h2 v = cvt_h2(w0, w1), z = cvt_h2(w0 - (float)v.x, w1 - (float)v.y);
+          w[0][p][i] = v.x, w[0][p][i + 1] = v.y;
+          w[PARTS - 1][p][i] = z.x, w[PARTS - 1][p][i + 1] = z.y;
+        }
+      }
+    }
+  }
+  // (fp16 weights only) those of a group whose values are scaled less than the accumulators
+  __device__ __forceinline__ void weights_down(const Scales& c, h8 (&w)[PARTS][2]) const {
+    if constexpr (PARTS == 1) {
+      if (__builtin_expect(min(c.ve[0], c.ve[1]) != vexp, 0)) {      // vexp is the larger of the two, or more
+        w[0][0] *= (_Float16)pow2i(c.ve[0] - vexp);
+        w[0][1] *= (_Float16)pow2i(c.ve[1] - vexp);
+      }
+    }
+  }
+
+  // Outputs, or the partial of span `span` of unit `unit`.
+  __device__ __forceinline__ void finish(const RowsArgs& a, const Unit& u, uint32_t unit, uint32_t span,
+                                         int half) {
+    if (!busy) return;
+    float lo, hi;
+    halves(l, lo, hi);
+    l = lo + hi;
+    const bool none = m == kNoScore;                     // no token, or no score that is a number
+    const float up = none ? 0.0f : pow2i(vexp);
+    if (a.n_split == 1) {
+      const float inv = none ? 0.0f : 1.0f / l;
+      float y[D / 2];
+#pragma unroll
+      for (int i = 0; i < D / 2; ++i) y[i] = none ? 0.0f : acc[i / 16][i % 16] * inv * up;
+      const uint64_t at = (uint64_t)u.b * a.o_stride[0] + (uint64_t)(u.h * a.G + g) * a.o_stride[1] +
+                          (uint64_t)j * a.o_stride[2];
+      store_row<D>(a, at, y, half, on);
+      return;
+    }
+    if (!on) return;
+    const uint64_t part = ((uint64_t)unit * a.n_split + span) * a.unit_rows + in_unit;
+#pragma unroll
+    for (int i = 0; i < D / 2; i += 4) {
+      const int e = 32 * (i / 16) + 8 * ((i % 16) / 4) + 4 * half;
+      float4 v;
+      v.x = acc[i / 16][i % 16] * up;
+      v.y = acc[i / 16][i % 16 + 1] * up;
+      v.z = acc[i / 16][i % 16 + 2] * up;
+      v.w = acc[i / 16][i % 16 + 3] * up;
+      *(float4*)(a.ws_acc + part * D + e) = none ? make_float4(0, 0, 0, 0) : v;
+    }
+    if (half == 0) *(float2*)(a.ws_ml + part * 2) = make_float2(m, none ? 0.0f : l);
+  }
+};
+
+// A wave's place in the call, the codes under way, and where its lanes find operands in a tile.
+template <int D, int WAVES, int PARTS>
+struct RowsWave {
+  using S = Shape<D, WAVES, PARTS>;
+  const RowsArgs& a;
+  Unit u;
+  uint32_t wave, bh, unit, span, t0, t1;        // the span's tiles [t0, t1)
+  int lane, half;
+  uint32_t blk0 = 0, blk = 0;                   // lane i: the pool block of block blk0 + i
+  RawCodes raw[S::TASKS];
+  uint32_t ka, va;                              // places of chunk 0 in a tile of keys and of values
+
+  __device__ __forceinline__ RowsWave(const RowsArgs& args) : a(args) {
+    wave = WAVES == 1 ? 0u : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    lane = threadIdx.x % kWave;
+    half = lane >> 5;
+  }
+
+  // Finds the workgroup's unit and span; false where it has none.
+  __device__ __forceinline__ bool start() {
+    // units with the most tokens first (the last rows see the most), a unit's spans together; the
+    // (sequence, KV head) goes round the XCDs, so that its units meet in one L2
+    const uint32_t heads = a.B * a.H;
+    bh = blockIdx.x % heads;
+    const uint32_t rest = blockIdx.x / heads;
+    span = rest % a.n_split;
+    unit = (a.n_rb - 1 - rest / a.n_split) * heads + bh;
+    u = unit_at(a, unit);
+    if (u.rb * a.unit_rows >= u.rows) return false;
+    const uint32_t tiles = (u.tokens + S::TILE - 1) / S::TILE;
+    const uint32_t spans = row_spans(tiles, a.n_split, a.min_tiles);
+    if (span >= spans) return false;
+    t0 = span_start(tiles, spans, span);
+    t1 = span_start(tiles, spans, span + 1);
+    // Chunk 2 k + half of a key's row lies at ka ^ 32 k, and column piece (lane's) of element block mb
+    // of values at va ^ 64 mb, for tokens 8 on at (va ^ 16 ^ 64 mb) + 8 rows.
+    ka = (lane & 31) * S::ROW + 16u * key_chunk<D>(half, lane & 31);
+    const uint32_t tk = 4 * half + (((uint32_t)lane >> 2) & 3u);
+    const uint32_t chunk = 2 * (((uint32_t)lane >> 4) & 1u) + (((uint32_t)lane >> 1) & 1u);
+    va = tk * S::ROW + 16u * (chunk ^ value_swap<D>(tk)) + 8u * (lane & 1);
+    return true;
+  }
+
+  __device__ __forceinline__ void load_blocks(uint32_t first) {
     blk0 = first;
     uint32_t i = first + (uint32_t)lane;
     bool ok = true;
@@ -440,10 +588,9 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 1 ? 2 : 2) void rows_kernel
     ok = ok && i < a.pg.max_blocks;
     const uint32_t p = ok ? (uint32_t)a.pg.table[(size_t)u.b * a.pg.max_blocks + i] : 0u;
     blk = p < a.pg.n_blocks ? p : 0u;
-  };
-  const uint32_t sub = (uint32_t)lane % S::LPV, vec = (uint32_t)lane / S::LPV;
-  RawCodes raw[S::TASKS];
-  auto load_tile = [&](uint32_t tile) __attribute__((always_inline)) {
+  }
+
+  __device__ __forceinline__ void load_tile(uint32_t tile) {
 #pragma unroll
     for (int k = 0; k < S::TASKS; ++k) {
       const uint32_t task = wave + WAVES * k;
@@ -452,7 +599,7 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 1 ? 2 : 2) void rows_kernel
       // a group past the last token reads the last group's, a token past it the last token's
       uint32_t first = tile * S::TILE + (task % S::NG) * S::GROUP;
       first = min(first, (u.tokens - 1) / S::GROUP * S::GROUP);
-      const uint32_t jj = min(vec, u.tokens - 1 - first);
+      const uint32_t jj = min((uint32_t)lane / S::LPV, u.tokens - 1 - first);
       uint32_t slot0 = (u.b * a.H + u.h) * a.cap + first;
       if (a.pg.table) {
         const uint32_t i = first >> a.pg.block_log2;
@@ -460,210 +607,270 @@ __global__ __launch_bounds__(WAVES * kWave, WAVES == 1 ? 2 : 2) void rows_kernel
         const uint32_t p = (uint32_t)__builtin_amdgcn_readlane((int)blk, (int)(i - blk0));
         slot0 = ((p * a.H + u.h) << a.pg.block_log2) + (first & ((1u << a.pg.block_log2) - 1u));
       }
-      raw[k] = load_raw(a, kind, D, slot0, jj, sub);
+      raw[k] = load_raw(a, kind, D, slot0, jj, (uint32_t)lane % S::LPV);
     }
-  };
-  auto rebuild_tile = [&](int buf) __attribute__((always_inline)) {
+  }
+
+  // The codes under way into the tile at `tile` (keys, then values), their E's into `exps`.
+  __device__ __forceinline__ void rebuild_tile(const char* lut, char* tile, int* exps) {
 #pragma unroll
     for (int k = 0; k < S::TASKS; ++k) {
       const uint32_t task = wave + WAVES * k;
       if (2 * S::NG % WAVES != 0 && task >= 2 * S::NG) continue;
       const int kind = (int)(task / S::NG);
-      const uint32_t group = task % S::NG, t = group * S::GROUP + vec;
+      const uint32_t t = task % S::NG * S::GROUP + (uint32_t)lane / S::LPV;
       const uint32_t swap = kind == 0 ? key_chunk<D>(0, t) : value_swap<D>(t);
-      const int e = rebuild<D, PARTS>(raw[k], a.n[kind], a.log_norms[kind] != 0, s_lut[kind],
-                                      s_tile[buf][kind] + t * S::ROW, S::PLANE, sub, swap);
-      if (lane == 0) s_exp[buf][kind][group] = e;
+      const int e = rebuild<D, PARTS>(raw[k], a.n[kind], a.log_norms[kind] != 0, lut + kind * S::LUT,
+                                      tile + kind * S::KIND + t * S::ROW, S::PLANE,
+                                      (uint32_t)lane % S::LPV, swap);
+      if (lane == 0) exps[kind * S::NG + task % S::NG] = e;
     }
-  };
+  }
 
-  float m = kNoScore, l = 0.0f;
-  int vexp = kNoExp;                                     // E of the accumulators
-  v16f acc[D / 32];
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) acc[i] = (v16f)(0.0f);
+  __device__ __forceinline__ void load_tables(char* lut) {
+    for (int kind = 0; kind < 2; ++kind)
+      for (uint32_t i = threadIdx.x; i < a.n[kind]; i += WAVES * kWave) {
+        const float2 cs = ((const float2*)a.lut[kind])[i];
+        if constexpr (PARTS == 1) ((h2*)(lut + kind * S::LUT))[i] = cvt_h2(cs.x, cs.y);
+        else ((float2*)(lut + kind * S::LUT))[i] = cs;
+      }
+  }
 
-  // the lane's places in a tile of keys (its token's row, by k) and of values (by element block and
-  // half of the 16 tokens)
-  uint32_t ka[D / 16], va[D / 32][2];
-#pragma unroll
-  for (int k = 0; k < D / 16; ++k)
-    ka[k] = (lane & 31) * S::ROW + 16u * key_chunk<D>(2 * k + half, lane & 31);
-#pragma unroll
-  for (int mb = 0; mb < D / 32; ++mb)
+  // Operands of 32 tokens whose keys or values begin at `at`.
+  __device__ __forceinline__ h8 key(const char* at, int k) const {
+    return read_h8(at + (ka ^ (32u * k)));
+  }
+  __device__ __forceinline__ h8 value(const char* at, int mb) const {
+    h8 v;
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      const uint32_t tk = 8 * z + 4 * half + (((uint32_t)lane >> 2) & 3u);
-      const uint32_t chunk = 4 * mb + 2 * (((uint32_t)lane >> 4) & 1u) + (((uint32_t)lane >> 1) & 1u);
-      va[mb][z] = tk * S::ROW + 16u * (chunk ^ value_swap<D>(tk)) + 8u * (lane & 1);
+      const s4 c = read_columns(at + ((va ^ (16u * z) ^ (64u * mb)) + 8u * z * S::ROW));
+      __builtin_memcpy((char*)&v + 8 * z, &c, 8);
     }
-
-  // 32 tokens from `tb` on, at offset `part` of the tile in `buf`
-  auto work32 = [&](auto buf_c, auto part_c, uint32_t tb) __attribute__((always_inline)) {
-    constexpr int buf = decltype(buf_c)::value, part = decltype(part_c)::value;
-    // ---- scores ----
-    const char* const kt = s_tile[buf][0] + 32 * part * S::ROW;
-    v16f s = (v16f)(0.0f);
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-      const h8 kh = read_h8(kt + ka[k]);
-      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh, q[0][k], s, 0, 0, 0);
-      if constexpr (PARTS == 2) {
-        const h8 kl = read_h8(kt + ka[k] + S::PLANE);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh, q[1][k], s, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kl, q[0][k], s, 0, 0, 0);
-      }
-    }
-    // registers 0 .. 7 hold the tokens of the first group of 16, 8 .. 15 those of the second
-    if (tb + 32 > lim_lo) {
-      const uint32_t t = tb + 4 * half;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = t + (i % 4) + 8 * (i / 4) < lim ? s[i] : -INFINITY;
-    }
-    float f[2], top = -INFINITY;
-    int ve[2];
+    return v;
+  }
+  __device__ __forceinline__ static Scales scales(const int* exps, int part) {
+    Scales c;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const int group = (32 * part + 16 * p) / S::GROUP;
-      f[p] = fmaxf(qf * pow2i(__builtin_amdgcn_readfirstlane(s_exp[buf][0][group])), FLT_MIN);
-      ve[p] = __builtin_amdgcn_readfirstlane(s_exp[buf][1][group]);
-      float mx = s[8 * p];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[8 * p + i]);
-      top = fmaxf(top, mx * f[p]);
+      c.ke[p] = __builtin_amdgcn_readfirstlane(exps[group]);
+      c.ve[p] = __builtin_amdgcn_readfirstlane(exps[S::NG + group]);
     }
-    if (__builtin_amdgcn_ballot_w64(top > m + (kLazy + kBias)) != 0) {
-      float lo, hi;
-      halves(top, lo, hi);
-      // rows that stay below keep their reference: a row's bits do not depend on its neighbours
-      const float most = fmaxf(lo, hi);
-      const float mn = most > m + (kLazy + kBias) ? most - kBias : m;
-      const float down = __builtin_amdgcn_exp2f(m - mn);
-      l *= down;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) acc[i] *= down;
-      m = mn;
-    }
-    const int vmax = max(ve[0], ve[1]);
-    if (vmax > vexp) {
-      const float down = pow2i(vexp - vmax);
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) acc[i] *= down;
-      vexp = vmax;
-    }
-    // ---- weights (their sum is that of the rounded ones) and values, 16 tokens at a time ----
-    const char* const vt = s_tile[buf][1] + 32 * part * S::ROW;
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      h8 ph, pl;
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * p + i], f[p], -m));
-        float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * p + i + 1], f[p], -m));
-        if constexpr (PARTS == 1) {
-          const h2 v = cvt_h2(w0, w1);
-          l = __builtin_amdgcn_fdot2(v, (h2){(_Float16)1.0f, (_Float16)1.0f}, l, false);
-          ph[i] = v.x, ph[i + 1] = v.y;
-        } else {
-          l += w0 + w1;
-          if (ve[p] != vexp) {
-            const float down = pow2i(ve[p] - vexp);
-            w0 *= down, w1 *= down;
-          }
-          const h2 v = cvt_h2(w0, w1), z = cvt_h2(w0 - (float)v.x, w1 - (float)v.y);
-          ph[i] = v.x, ph[i + 1] = v.y;
-          pl[i] = z.x, pl[i + 1] = z.y;
-        }
-      }
-      if constexpr (PARTS == 1)
-        if (ve[p] != vexp) ph *= (_Float16)pow2i(ve[p] - vexp);
-#pragma unroll
-      for (int mb = 0; mb < D / 32; ++mb) {
-        h8 vh, vl;
-#pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          const char* const at = vt + va[mb][z] + 16 * p * S::ROW;
-          const s4 c = read_columns(at);
-          __builtin_memcpy((char*)&vh + 8 * z, &c, 8);
-          if constexpr (PARTS == 2) {
-            const s4 cl = read_columns(at + S::PLANE);
-            __builtin_memcpy((char*)&vl + 8 * z, &cl, 8);
-          }
-        }
-        acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, ph, acc[mb], 0, 0, 0);
-        if constexpr (PARTS == 2) {
-          acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh, pl, acc[mb], 0, 0, 0);
-          acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vl, ph, acc[mb], 0, 0, 0);
-        }
-      }
-    }
-  };
-  auto work = [&](auto buf_c, uint32_t tile) __attribute__((always_inline)) {
-    const uint32_t tb = tile * S::TILE;
-    if (busy && tb < lim_hi) work32(buf_c, std::integral_constant<int, 0>{}, tb);
-    if constexpr (S::TILE > 32)
-      if (busy && tb + 32 < lim_hi) work32(buf_c, std::integral_constant<int, 1>{}, tb + 32);
-  };
-
-  if (t0 < t1) {
-    if (a.pg.table) load_blocks((t0 * S::TILE) >> a.pg.block_log2);
-    load_tile(t0);
+    return c;
   }
-  if constexpr (S::BUFS == 1) {
-    for (uint32_t t = t0; t < t1; ++t) {
+};
+
+// Every workgroup rebuilds its own tiles; 32 rows a wave.  Eight waves have two tiles in LDS and
+// rebuild the next before they use the current one, one wait a tile; fewer waves, several of whose
+// workgroups share a compute unit, rebuild a tile and then use it.
+template <int D, int WAVES, int PARTS>
+__global__ __launch_bounds__(WAVES * kWave, 2) void rows_kernel(RowsArgs a) {
+  using S = Shape<D, WAVES, PARTS>;
+  constexpr int BUFS = WAVES == 8 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) char s_lut[2 * S::LUT];
+  __shared__ __attribute__((aligned(1024))) char s_tile[BUFS][2 * S::KIND];
+  __shared__ int s_exp[BUFS][2 * S::NG];
+  RowsWave<D, WAVES, PARTS> w(a);
+  if (!w.start()) return;
+  w.load_tables(s_lut);
+  Rows<D, PARTS> r;
+  r.start(a, w.u, 32 * w.wave, w.lane);
+  if (w.t0 < w.t1) {
+    if (a.pg.table) w.load_blocks((w.t0 * S::TILE) >> a.pg.block_log2);
+    w.load_tile(w.t0);
+  }
+  auto work = [&](auto buf_c, uint32_t t) __attribute__((always_inline)) {
+    constexpr int buf = decltype(buf_c)::value;
+#pragma unroll
+    for (int part = 0; part < S::TILE / 32; ++part) {
+      const uint32_t tb = t * S::TILE + 32 * part;
+      if (!r.busy || tb >= r.lim_hi) continue;
+      const char* const kt = s_tile[buf] + 32 * part * S::ROW;
+      const char* const vt = kt + S::KIND;
+      v16f s = (v16f)(0.0f);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        const h8 h = w.key(kt, k);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(h, r.q[0][k], s, 0, 0, 0);
+        if constexpr (PARTS == 2) {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_f16(h, r.q[1][k], s, 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_32x32x16_f16(w.key(kt + S::PLANE, k), r.q[0][k], s, 0, 0, 0);
+        }
+      }
+      const Scales c = w.scales(s_exp[buf], part);
+      r.settle(s, c, tb, w.half);
+      h8 p[PARTS][2];
+      r.weigh(s, c, p);
+      r.weights_down(c, p);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int mb = 0; mb < D / 32; ++mb) {
+          const h8 h = w.value(vt + 16 * i * S::ROW, mb);
+          r.acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h, p[0][i], r.acc[mb], 0, 0, 0);
+          if constexpr (PARTS == 2) {
+            const h8 g = w.value(vt + 16 * i * S::ROW + S::PLANE, mb);
+            r.acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(h, p[1][i], r.acc[mb], 0, 0, 0);
+            r.acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g, p[0][i], r.acc[mb], 0, 0, 0);
+          }
+        }
+    }
+  };
+  const std::integral_constant<int, 0> c0;
+  if constexpr (BUFS == 1) {
+    for (uint32_t t = w.t0; t < w.t1; ++t) {
       __syncthreads();                                   // the tables; the last tile's reads
-      rebuild_tile(0);
-      if (t + 1 < t1) load_tile(t + 1);
+      w.rebuild_tile(s_lut, s_tile[0], s_exp[0]);
+      if (t + 1 < w.t1) w.load_tile(t + 1);
       __syncthreads();
-      work(std::integral_constant<int, 0>{}, t);
+      work(c0, t);
     }
   } else {
-    // two tiles a round, so that the places in LDS are known when it is compiled
+    const std::integral_constant<int, 1> c1;
     auto step = [&](auto buf_c, uint32_t t) __attribute__((always_inline)) {
-      if (t + 1 < t1) rebuild_tile(decltype(buf_c)::value ^ 1);
-      if (t + 2 < t1) load_tile(t + 2);
+      constexpr int other = 1 - decltype(buf_c)::value;
+      if (t + 1 < w.t1) w.rebuild_tile(s_lut, s_tile[other], s_exp[other]);
+      if (t + 2 < w.t1) w.load_tile(t + 2);
       work(buf_c, t);
       __syncthreads();
     };
     __syncthreads();
-    if (t0 < t1) rebuild_tile(0);
-    if (t0 + 1 < t1) load_tile(t0 + 1);
+    if (w.t0 < w.t1) w.rebuild_tile(s_lut, s_tile[0], s_exp[0]);
+    if (w.t0 + 1 < w.t1) w.load_tile(w.t0 + 1);
     __syncthreads();
-    for (uint32_t t = t0; t < t1; t += 2) {
-      step(std::integral_constant<int, 0>{}, t);
-      if (t + 1 < t1) step(std::integral_constant<int, 1>{}, t + 1);
+    for (uint32_t t = w.t0; t < w.t1; t += 2) {          // so that the places in LDS are constants
+      step(c0, t);
+      if (t + 1 < w.t1) step(c1, t + 1);
     }
   }
-  if (!busy) return;
+  r.finish(a, w.u, w.unit, w.span, w.half);
+}
 
-  float lo, hi;
-  halves(l, lo, hi);
-  l = lo + hi;
-  float y[D / 2];
-  const bool none = m == kNoScore;                       // no token, or no score that is a number
-  const float up = none ? 0.0f : pow2i(vexp);
-  if (a.n_split == 1) {
-    const float inv = none ? 0.0f : 1.0f / l;
+// The tiles of a call's tokens, rebuilt once into the workspace as rows_many_kernel holds them in LDS,
+// with their E's: a tile per workgroup, by way of LDS so that whole cache lines are stored.
+template <int D>
+__global__ __launch_bounds__(kBlockThreads) void rows_tiles_kernel(RowsArgs a) {
+  using S = Shape<D, 4, 1>;
+  __shared__ __attribute__((aligned(16))) char s_lut[2 * S::LUT];
+  __shared__ __attribute__((aligned(1024))) char s_tile[2 * S::KIND];
+  __shared__ int s_exp[2 * S::NG];
+  RowsWave<D, 4, 1> w(a);
+  const uint32_t heads = a.B * a.H;
+  w.bh = blockIdx.x % heads;
+  const uint32_t tile = blockIdx.x / heads;
+  w.u = unit_at(a, (a.n_rb - 1) * heads + w.bh);         // the last rows see the most
+  if (tile * S::TILE >= w.u.tokens) return;
+  if (a.pg.table) w.load_blocks((tile * S::TILE) >> a.pg.block_log2);
+  w.load_tile(tile);
+  w.load_tables(s_lut);
+  __syncthreads();
+  w.rebuild_tile(s_lut, s_tile, s_exp);
+  __syncthreads();
+  const uint64_t at = (uint64_t)w.bh * a.n_tiles + tile;
+  char* const out = a.ws_tiles + at * (2 * S::KIND);
 #pragma unroll
-    for (int i = 0; i < D / 2; ++i) y[i] = none ? 0.0f : acc[i / 16][i % 16] * inv * up;
-    const uint64_t at = (uint64_t)u.b * a.o_stride[0] + (uint64_t)(u.h * a.G + g) * a.o_stride[1] +
-                        (uint64_t)j * a.o_stride[2];
-    store_row<D>(a, at, y, half, on);
-    return;
-  }
-  if (!on) return;
-  const uint64_t part = ((uint64_t)unit * a.n_split + span) * (WAVES * 32) + wave * 32 + (lane & 31);
+  for (uint32_t i = threadIdx.x * 16; i < 2 * S::KIND; i += kBlockThreads * 16)
+    *(u32x4a*)(out + i) = *(const u32x4a*)(s_tile + i);
+  if (threadIdx.x < 2 * S::NG) a.ws_exps[at * (2 * S::NG) + threadIdx.x] = s_exp[threadIdx.x];
+}
+
+// Eight waves on rebuilt tiles, three of them in LDS.  The steps of 32 tokens i overlap: the score
+// products of i + 1 are issued between the exponentials of i (beside an MFMA of 32 cycles five or six
+// vector instructions run, of the same wave too), and every operand is read from LDS a phase before
+// its products: the keys of i + 2 before the value products of i, the values of i + 1 after them.
+// In the middle of tile t the waves meet: tile t + 1 is then complete and tile t - 1 read, and its
+// place is taken by t + 2, which was requested a tile before.
+template <int D>
+__global__ __launch_bounds__(8 * kWave, 2) void rows_many_kernel(RowsArgs a) {
+  using S = Shape<D, 8, 1>;
+  constexpr uint32_t SLOT = 2 * S::KIND, THREADS = 8 * kWave, EACH = SLOT / (THREADS * 16);
+  __shared__ __attribute__((aligned(1024))) char s_tile[3 * SLOT];
+  __shared__ int s_exp[3][2 * S::NG];
+  RowsWave<D, 8, 1> w(a);
+  if (!w.start()) return;
+  Rows<D, 1> r;
+  r.start(a, w.u, 32 * w.wave, w.lane);
+  const uint64_t tile0 = (uint64_t)w.bh * a.n_tiles;
+  u32x4a moved[EACH];
+  int moved_exp = 0;
+  const bool has_exp = threadIdx.x < 2 * S::NG;
+  auto fetch = [&](uint32_t tile) __attribute__((always_inline)) {
+    const char* const src = a.ws_tiles + (tile0 + tile) * SLOT + threadIdx.x * 16;
 #pragma unroll
-  for (int i = 0; i < D / 2; i += 4) {
-    const int e = 32 * (i / 16) + 8 * ((i % 16) / 4) + 4 * half;
-    float4 v;
-    v.x = acc[i / 16][i % 16] * up;
-    v.y = acc[i / 16][i % 16 + 1] * up;
-    v.z = acc[i / 16][i % 16 + 2] * up;
-    v.w = acc[i / 16][i % 16 + 3] * up;
-    *(float4*)(a.ws_acc + part * D + e) = none ? make_float4(0, 0, 0, 0) : v;
+    for (uint32_t i = 0; i < EACH; ++i) moved[i] = *(const u32x4a*)(src + i * (THREADS * 16));
+    if (has_exp) moved_exp = a.ws_exps[(tile0 + tile) * (2 * S::NG) + threadIdx.x];
+  };
+  auto place = [&](uint32_t slot) __attribute__((always_inline)) {
+    char* const dst = s_tile + slot * SLOT + threadIdx.x * 16;
+#pragma unroll
+    for (uint32_t i = 0; i < EACH; ++i) *(u32x4a*)(dst + i * (THREADS * 16)) = moved[i];
+    if (has_exp) s_exp[slot][threadIdx.x] = moved_exp;
+  };
+  if (w.t0 < w.t1) {
+    fetch(w.t0);
+    place(0);
   }
-  if (half == 0) *(float2*)(a.ws_ml + part * 2) = make_float2(m, none ? 0.0f : l);
+  if (w.t0 + 1 < w.t1) {
+    fetch(w.t0 + 1);
+    place(1);
+  }
+  if (w.t0 + 2 < w.t1) fetch(w.t0 + 2);
+  __syncthreads();
+
+  h8 kh[D / 16], p[1][2];
+  auto read_keys = [&](const char* at) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) kh[k] = w.key(at, k);
+  };
+  auto scores = [&]() __attribute__((always_inline)) {
+    v16f x = (v16f)(0.0f);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+      x = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh[k], r.q[0][k], x, 0, 0, 0);
+    return x;
+  };
+
+  read_keys(s_tile);
+  v16f s = scores();
+  read_keys(s_tile + 32 * S::ROW);
+  uint32_t slot = 0;                                     // of tile t
+  for (uint32_t t = w.t0; t < w.t1; ++t) {
+    const uint32_t next = slot == 2 ? 0u : slot + 1, after = next == 2 ? 0u : next + 1;
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      const char* const vt = s_tile + slot * SLOT + S::KIND + 32 * part * S::ROW;
+      const Scales c = w.scales(s_exp[slot], part);
+      r.settle(s, c, t * S::TILE + 32 * part, w.half);
+      const v16f s1 = scores();                          // past the last tile: of what lies there, unused
+      r.weigh(s, c, p);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);             // an MFMA,
+        __builtin_amdgcn_sched_group_barrier(0x2, 768 / D, 0);       // vector instructions
+      }
+      r.weights_down(c, p);
+      s = s1;
+      if (part == 0) {
+        __syncthreads();
+        if (t + 2 < w.t1) place(after);
+        if (t + 3 < w.t1) fetch(t + 3);
+      }
+      h8 vh[2][D / 32];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int mb = 0; mb < D / 32; ++mb) vh[i][mb] = w.value(vt + 16 * i * S::ROW, mb);
+      read_keys(s_tile + next * SLOT + 32 * part * S::ROW);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int mb = 0; mb < D / 32; ++mb)
+          r.acc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vh[i][mb], p[0][i], r.acc[mb], 0, 0, 0);
+    }
+    slot = next;
+  }
+  r.finish(a, w.u, w.unit, w.span, w.half);
 }
 
 // The spans of one row, a row per wave, its elements across the lanes: M = max m, then
@@ -741,11 +948,16 @@ template <int D>
 int launch(const RowsArgs& a, unsigned waves, bool wide, hipStream_t s) {
   const uint64_t units = (uint64_t)a.B * a.H * a.n_rb;
   const dim3 grid((unsigned)(units * a.n_split)), block(waves * kWave);
+  if (a.ws_tiles) {
+    hipLaunchKernelGGL((rows_tiles_kernel<D>), dim3(a.B * a.H * a.n_tiles), dim3(4 * kWave), 0, s, a);
+    if (hipGetLastError() != hipSuccess) return -2;
+  }
   if (waves == 1) {
     if (wide) hipLaunchKernelGGL((rows_kernel<D, 1, 2>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((rows_kernel<D, 1, 1>), grid, block, 0, s, a);
   } else if (waves == 8) {
     if (wide) hipLaunchKernelGGL((rows_kernel<D, 8, 2>), grid, block, 0, s, a);
+    else if (a.ws_tiles) hipLaunchKernelGGL((rows_many_kernel<D>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((rows_kernel<D, 8, 1>), grid, block, 0, s, a);
   } else {
     if (wide) hipLaunchKernelGGL((rows_kernel<D, 4, 2>), grid, block, 0, s, a);

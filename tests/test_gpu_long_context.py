@@ -108,6 +108,11 @@ PREFILL = [
     (64, 4, 1, "swapped", 256, 2, 512, [300, 257], 129, None),
     (64, 1, 2, "early8", 128, 2, 256, [256, -7], 16, [-1, 16]),
     (64, 1, 5, "boost", 64, 3, 192, [190, 1], 13, [13, 1]),
+    # many rows per KV head: bf16 outputs take tiles that are rebuilt once
+    (128, 1, 4, "base", 64, 12, 768, [768, 333, 0, 64], 260, [260, 100, 5, 70]),
+    (128, 2, 16, "log", 32, 7, 224, [224], 66, None),
+    (64, 2, 8, "swapped", 128, 6, 700, [768, 129], 130, [130, 129]),
+    (64, 1, 32, "early8", 32, 3, 96, [95, 1, 33], 33, [33, 1, 0]),
 ]
 
 
@@ -130,7 +135,8 @@ def test_prefill_paged(gpu, case, q_dtype, o_dtype):
                    d ** -0.5, f"prefill {case[:5]} {q_dtype}->{o_dtype}")
 
 
-@pytest.mark.parametrize("d,T,G", [(128, 3, 4), (128, 70, 4), (64, 3, 4), (64, 150, 2)])
+@pytest.mark.parametrize("d,T,G", [(128, 3, 4), (128, 70, 4), (64, 3, 4), (64, 150, 2), (128, 290, 4),
+                                   (64, 130, 8), (128, 30, 4), (64, 25, 3)])
 @pytest.mark.parametrize("o_dtype", ["bf16", "f32"])
 def test_prefill_split_and_scales(gpu, d, T, G, o_dtype):
     """A context of several thousand tokens (its spans are merged), with vectors of very different
