@@ -64,7 +64,7 @@ TVQ_ROWS_HOST_DEVICE uint32_t span_start(uint32_t tiles, uint32_t n, uint32_t k)
 }
 
 struct RowsPlan {
-  uint32_t waves;        // of a workgroup: 1, 4 or 8
+  uint32_t waves;        // of a workgroup: 4 or 8
   uint32_t unit_rows, tile, n_rb, n_split, min_tiles;
   int64_t units, acc_bytes, ml_bytes;
   int64_t n_tiles, tile_bytes, exp_bytes;   // rebuilt tiles (0: none)
@@ -79,30 +79,33 @@ constexpr int64_t kRebuildBytes = 1ll << 31;         // and the most they may ta
 // batch, heads: of the cache; rows: query rows of a (sequence, KV head); tokens: bound of a
 // context; d: head dimension; cus: compute units.
 //
-// Up to 32 rows a wave works by itself, with its own tile in LDS; above, four waves share a tile.
-// The spans of a launch go to the places that the device has for its workgroups (8 single waves or
-// 2 workgroups of four a compute unit), so many at a time; a span costs its tiles and, for its start
-// and its partial, about kSpanTiles more.  The number of spans with the least time for full
-// contexts is taken, of at least 128 or 256 tokens each.
+// Up to 32 rows the four waves of a workgroup take tokens of their own, in tiles of 32 (units of 16 or
+// 32 rows); above, four or eight waves of 32 rows each share tiles of 64.
+// The spans of a launch go to the places that the device has for its workgroups, so many at a time;
+// a span costs its tiles and, for its start and its partial, about kSpanTiles more.  The number of
+// spans with the least time for full contexts is taken, of at least 4 tiles each (one a wave where
+// the waves take tokens of their own).
 constexpr int64_t kSpanTiles = 3;
 
 inline RowsPlan rows_plan(int64_t batch, int64_t heads, int64_t rows, int64_t tokens, int32_t d,
                           int64_t cus) {
   const auto ceil_div = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
   RowsPlan p;
-  p.waves = rows <= 32 ? 1 : rows <= 128 ? 4 : 8;
-  p.unit_rows = p.waves * 32;
-  p.tile = p.waves == 1 ? 32 : 64;
+  const bool few = rows <= 32;
+  p.waves = rows <= 128 ? 4 : 8;
+  p.unit_rows = rows <= 16 ? 16 : few ? 32 : p.waves * 32;
+  p.tile = few ? 32 : 64;
   p.min_tiles = 4;
   const int64_t n_rb = ceil_div(rows, p.unit_rows);
   p.n_rb = (uint32_t)n_rb;
   p.units = batch * heads * n_rb;
-  const int64_t places = cus * (p.waves == 1 ? 8 : p.waves == 4 ? 2 : 1);
+  const int64_t places = cus * (p.waves == 8 ? 1 : p.unit_rows == 16 ? 3 : 2);
   const int64_t tiles = ceil_div(tokens, p.tile);
   const int64_t fill = 4 * places / p.units + 1;      // past four rounds of places nothing is gained
   const int64_t most = tokens / (p.min_tiles * (int64_t)p.tile);
   const auto time = [&](int64_t n) {
-    return ceil_div(p.units * n, places) * (ceil_div(tiles, n) + (n > 1 ? kSpanTiles : 0));
+    return ceil_div(p.units * n, places) *
+           (ceil_div(tiles, few ? 4 * n : n) + (n > 1 ? kSpanTiles : 0));
   };
   int64_t best = 1;
   for (int64_t n = 2; n <= most && n <= fill; ++n)

@@ -81,6 +81,19 @@ __device__ __forceinline__ void halves(float x, float& lo, float& hi) {
   hi = __uint_as_float(r[1]);
 }
 
+// f over the values of the LPR lanes that hold a row (lane bits 5 and, of four, 4).
+template <int LPR, class F>
+__device__ __forceinline__ float over_row(float x, F f) {
+  if constexpr (LPR == 4) {
+    const uint32_t u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  float lo, hi;
+  halves(x, lo, hi);
+  return f(lo, hi);
+}
+
 // 2^e as fp32; 0 below the normal range.
 __device__ __forceinline__ float pow2i(int e) {
   return e < -126 ? 0.0f : __uint_as_float((uint32_t)(min(e, 127) + 127) << 23);
@@ -119,7 +132,7 @@ template <int D, int WAVES, int PARTS>
 struct Shape {
   static constexpr int LPV = D / kElemsPerLane;          // lanes per token
   static constexpr int GROUP = kWave / LPV;              // tokens that a wave rebuilds at once
-  static constexpr int TILE = WAVES == 1 ? 32 : 64;      // tokens
+  static constexpr int TILE = 64;                        // tokens
   static constexpr int NG = TILE / GROUP;
   static constexpr int TASKS = (2 * NG + WAVES - 1) / WAVES;   // (kind, group) tasks of a wave
   static constexpr int ROW = 2 * D;                      // bytes of a token in a plane
@@ -179,13 +192,22 @@ __device__ __forceinline__ void angle_codes(const RawCodes& r, uint32_t odd, uin
   unpack16_index<W>(o, c);
 }
 
-// Rebuilds a lane's 16 pairs into the tile at `dst` (its token's row); returns E of the group.
+// Rebuilds a lane's 16 pairs into the tile at `dst` (its token's row); returns E of the group.  The
+// table reads go out first and return while the norms are computed.
 template <int D, int PARTS>
 __device__ __forceinline__ int rebuild(const RawCodes& raw, uint32_t n, bool log_norms,
-                                       const char* lut, char* dst, int plane, uint32_t sub,
+                                       const char* lut, char* dst, uint32_t plane, uint32_t sub,
                                        uint32_t swap) {
-  const float rmin = __uint_as_float(raw.hdr[0]), rmax = __uint_as_float(raw.hdr[1]);
+  using Entry = std::conditional_t<PARTS == 1, h2, float2>;        // cos, sin
+  Entry cs[16];
+  uint32_t c[16];
+  if (n == 64) angle_codes<6>(raw, 0, c);
+  else if (n == 128) angle_codes<7>(raw, sub & 1u, c);
+  else angle_codes<8>(raw, 0, c);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) cs[i] = ((const Entry*)lut)[c[i]];
   // E: the largest norm of the group's tokens (the lanes of a token hold the same)
+  const float rmin = __uint_as_float(raw.hdr[0]), rmax = __uint_as_float(raw.hdr[1]);
   int top = (int)raw.hdr[1];
   if constexpr (D == 64) top = max(top, (int)row_ror<2>((uint32_t)top));
   top = max(top, (int)row_ror<4>((uint32_t)top));
@@ -193,13 +215,6 @@ __device__ __forceinline__ int rebuild(const RawCodes& raw, uint32_t n, bool log
   top = max(max(__builtin_amdgcn_readlane(top, 0), __builtin_amdgcn_readlane(top, 16)),
             max(__builtin_amdgcn_readlane(top, 32), __builtin_amdgcn_readlane(top, 48)));
   const int e = min(max(((top >> 23) - 127) & ~7, -120), 120);
-  const float down = pow2i(-e);
-
-  uint32_t c[16];
-  if (n == 64) angle_codes<6>(raw, 0, c);
-  else if (n == 128) angle_codes<7>(raw, sub & 1u, c);
-  else angle_codes<8>(raw, 0, c);
-
   float r[16];
   if (log_norms) {
     const float lo = fmaxf(rmin, FLT_MIN), hi = fmaxf(rmax, FLT_MIN);
@@ -218,6 +233,7 @@ __device__ __forceinline__ int rebuild(const RawCodes& raw, uint32_t n, bool log
       r[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(q, step, base));
     }
   } else {
+    const float down = pow2i(-e);
     const float step = linear_step255(rmin, rmax) * down, base = rmin * down;
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -230,12 +246,10 @@ __device__ __forceinline__ int rebuild(const RawCodes& raw, uint32_t n, bool log
     for (int k = 0; k < 4; ++k) {
       const int i = 4 * j + k;
       if constexpr (PARTS == 1) {
-        const h2 cs = ((const h2*)lut)[c[i]];
         const h2 rr = cvt_h2(r[i & ~1], r[i | 1]);
-        hi[k] = h2_bits((i % 2 ? (h2){rr.y, rr.y} : (h2){rr.x, rr.x}) * cs);
+        hi[k] = h2_bits((i % 2 ? (h2){rr.y, rr.y} : (h2){rr.x, rr.x}) * cs[i]);
       } else {
-        const float2 cs = ((const float2*)lut)[c[i]];
-        const float x = r[i] * cs.x, y = r[i] * cs.y;
+        const float x = r[i] * cs[i].x, y = r[i] * cs[i].y;
         const h2 h = cvt_h2(x, y);
         hi[k] = h2_bits(h);
         lo[k] = h2_bits(cvt_h2(x - (float)h.x, y - (float)h.y));
@@ -323,15 +337,18 @@ __device__ __forceinline__ void store_row(const RowsArgs& a, uint64_t at, float 
   }
 }
 
-// q^ = scale W D q of the lane's row as fp16 parts, elements 16 k + 8 half + i at [k][i]; returns
-// the power of two that the scores must be multiplied by.
-template <int D, int PARTS>
-__device__ __forceinline__ float load_rows(const RowsArgs& a, uint64_t at, int half,
-                                           h8 (&q)[PARTS][D / 16]) {
-  float x[D / 2];
+// q^ = scale W D q of the lane's row as fp16 parts; LPR lanes of the wave hold a row (its place among
+// them is `part`), elements 8 LPR k + 8 part + i at [k][i].  Returns the power of two that the scores
+// must be multiplied by.
+template <int D, int PARTS, int LPR>
+__device__ __forceinline__ float load_rows(const RowsArgs& a, uint64_t at, int lane,
+                                           h8 (&q)[PARTS][D / (8 * LPR)]) {
+  constexpr int N = D / LPR;
+  const int part = lane / (kWave / LPR);
+  float x[N];
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k) {
-    const int e = 16 * k + 8 * half;
+  for (int k = 0; k < N / 8; ++k) {
+    const int e = 8 * LPR * k + 8 * part;
     const u32x4a s = *(const u32x4a*)(a.signs + e / 2);
     if (a.q_f32) {
       const float* p = (const float*)a.q + at + e;
@@ -350,26 +367,25 @@ __device__ __forceinline__ float load_rows(const RowsArgs& a, uint64_t at, int h
       }
     }
   }
-  stage_regs(x, 1);
-  stage_regs(x, 2);
-  stage_regs(x, 4);
-  stage_halves(x, half);
-  stage_regs(x, 8);
-  stage_regs(x, 16);
-  if constexpr (D == 128) stage_regs(x, 32);
+#pragma unroll
+  for (int h = 1; h < N; h <<= 1) stage_regs(x, h);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    if constexpr (LPR == 4) x[j] = fwht_stage<16>(x[j], lane);
+    x[j] = fwht_stage<32>(x[j], lane);
+  }
   float top = 0.0f;
 #pragma unroll
-  for (int i = 0; i < D / 2; ++i) {
+  for (int i = 0; i < N; ++i) {
     x[i] *= a.qscale;
     top = fmaxf(top, fabsf(x[i]));
   }
-  float lo, hi;
-  halves(top, lo, hi);
+  top = over_row<LPR>(top, [](float u, float v) { return fmaxf(u, v); });
   // largest element in [2^7, 2^8)
-  const int e = min(max((int)(__float_as_uint(fmaxf(lo, hi)) >> 23) - 127 - 7, -119), 120);
+  const int e = min(max((int)(__float_as_uint(top) >> 23) - 127 - 7, -119), 120);
   const float down = pow2i(-e);
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k) {
+  for (int k = 0; k < N / 8; ++k) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float v = x[8 * k + i] * down;
@@ -414,7 +430,7 @@ struct Rows {
     lim_hi = (uint32_t)__builtin_amdgcn_readlane((int)lim, 31);
     const uint64_t at = (uint64_t)u.b * a.q_stride[0] + (uint64_t)(u.h * a.G + g) * a.q_stride[1] +
                         (uint64_t)j * a.q_stride[2];
-    qf = load_rows<D, PARTS>(a, at, lane >> 5, q);
+    qf = load_rows<D, PARTS, 2>(a, at, lane, q);
     m = kNoScore;
     l = 0.0f;
     vexp = kNoExp;
@@ -547,7 +563,7 @@ struct RowsWave {
   uint32_t ka, va;                              // places of chunk 0 in a tile of keys and of values
 
   __device__ __forceinline__ RowsWave(const RowsArgs& args) : a(args) {
-    wave = WAVES == 1 ? 0u : __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     lane = threadIdx.x % kWave;
     half = lane >> 5;
   }
@@ -563,7 +579,7 @@ struct RowsWave {
     unit = (a.n_rb - 1 - rest / a.n_split) * heads + bh;
     u = unit_at(a, unit);
     if (u.rb * a.unit_rows >= u.rows) return false;
-    const uint32_t tiles = (u.tokens + S::TILE - 1) / S::TILE;
+    const uint32_t tiles = (u.tokens + a.tile - 1) / a.tile;
     const uint32_t spans = row_spans(tiles, a.n_split, a.min_tiles);
     if (span >= spans) return false;
     t0 = span_start(tiles, spans, span);
@@ -590,24 +606,27 @@ struct RowsWave {
     blk = p < a.pg.n_blocks ? p : 0u;
   }
 
+  // Codes of the group of tokens from `first` on: past the last token those of the last group, in it
+  // those of the last token.
+  __device__ __forceinline__ RawCodes load_group(int kind, uint32_t first) {
+    first = min(first, (u.tokens - 1) / S::GROUP * S::GROUP);
+    const uint32_t jj = min((uint32_t)lane / S::LPV, u.tokens - 1 - first);
+    uint32_t slot0 = (u.b * a.H + u.h) * a.cap + first;
+    if (a.pg.table) {
+      const uint32_t i = first >> a.pg.block_log2;
+      if (i - blk0 >= kWave) load_blocks(i);
+      const uint32_t p = (uint32_t)__builtin_amdgcn_readlane((int)blk, (int)(i - blk0));
+      slot0 = ((p * a.H + u.h) << a.pg.block_log2) + (first & ((1u << a.pg.block_log2) - 1u));
+    }
+    return load_raw(a, kind, D, slot0, jj, (uint32_t)lane % S::LPV);
+  }
+
   __device__ __forceinline__ void load_tile(uint32_t tile) {
 #pragma unroll
     for (int k = 0; k < S::TASKS; ++k) {
       const uint32_t task = wave + WAVES * k;
       if (2 * S::NG % WAVES != 0 && task >= 2 * S::NG) continue;
-      const int kind = (int)(task / S::NG);
-      // a group past the last token reads the last group's, a token past it the last token's
-      uint32_t first = tile * S::TILE + (task % S::NG) * S::GROUP;
-      first = min(first, (u.tokens - 1) / S::GROUP * S::GROUP);
-      const uint32_t jj = min((uint32_t)lane / S::LPV, u.tokens - 1 - first);
-      uint32_t slot0 = (u.b * a.H + u.h) * a.cap + first;
-      if (a.pg.table) {
-        const uint32_t i = first >> a.pg.block_log2;
-        if (i - blk0 >= kWave) load_blocks(i);
-        const uint32_t p = (uint32_t)__builtin_amdgcn_readlane((int)blk, (int)(i - blk0));
-        slot0 = ((p * a.H + u.h) << a.pg.block_log2) + (first & ((1u << a.pg.block_log2) - 1u));
-      }
-      raw[k] = load_raw(a, kind, D, slot0, jj, (uint32_t)lane % S::LPV);
+      raw[k] = load_group((int)(task / S::NG), tile * S::TILE + (task % S::NG) * S::GROUP);
     }
   }
 
@@ -873,6 +892,266 @@ __global__ __launch_bounds__(8 * kWave, 2) void rows_many_kernel(RowsArgs a) {
   r.finish(a, w.u, w.unit, w.span, w.half);
 }
 
+// o of a row whose rotated-domain sum lies across the lanes of the wave, elements EPL lane ...
+template <int D>
+__device__ __forceinline__ void store_across(const RowsArgs& a, const Unit& u, uint32_t row,
+                                             float (&x)[D / kWave], int lane) {
+  constexpr int EPL = D / kWave;
+  fwht_across_lanes<EPL>(x, lane);
+  apply_signs<EPL>(x, a.signs[(EPL * lane) / 2], lane);
+  const uint32_t j = row / a.G, g = row - j * a.G;
+  const uint64_t at = (uint64_t)u.b * a.o_stride[0] + (uint64_t)(u.h * a.G + g) * a.o_stride[1] +
+                      (uint64_t)j * a.o_stride[2] + EPL * lane;
+  if constexpr (EPL == 2) {
+    if (a.o_f32) *(float2*)((float*)a.o + at) = make_float2(x[0], x[1]);
+    else *(uint32_t*)((uint16_t*)a.o + at) = bf16x2_rne(x[0], x[1]);
+  } else {
+    if (a.o_f32) ((float*)a.o)[at] = x[0];
+    else ((uint16_t*)a.o)[at] = (uint16_t)(bf16x2_rne(x[0], 0.0f) & 0xFFFFu);
+  }
+}
+
+// 16 query rows, a row on the lanes l, l + 16, l + 32 and l + 48, for calls with few rows: as Rows on
+// v_mfma_f32_16x16x32_f16 (A 16 x 32, B 32 x 16: lane l gives row or column l % 16 and the k's
+// 8 (l / 16) ..; register i of the result is row 4 (l / 16) + i).  The scores of 32 tokens are two
+// results, tokens 4 (l / 16) + i and 16 more, which in this order are the 8 k's that the lane gives
+// to the value products.
+template <int D, int PARTS>
+struct FewRows {
+  typedef float v4f __attribute__((ext_vector_type(4)));
+  uint32_t lim, lim_lo;                         // tokens that the row sees; the fewest of the 16
+  h8 q[PARTS][D / 32];
+  float qf, m, l;
+  int vexp;
+  v4f acc[D / 16];
+
+  __device__ __forceinline__ void start(const RowsArgs& a, const Unit& u, uint32_t first, int lane) {
+    const uint32_t r = min(u.rb * a.unit_rows + first + (lane & 15), u.rows - 1);
+    const uint32_t j = r / a.G, g = r - j * a.G;
+    const int64_t seen = u.pos0 + j + 1;
+    lim = seen < 0 ? 0u : (uint32_t)seen;
+    lim_lo = (uint32_t)__builtin_amdgcn_readlane((int)lim, 0);
+    const uint64_t at = (uint64_t)u.b * a.q_stride[0] + (uint64_t)(u.h * a.G + g) * a.q_stride[1] +
+                        (uint64_t)j * a.q_stride[2];
+    qf = load_rows<D, PARTS, 4>(a, at, lane, q);
+    m = kNoScore;
+    l = 0.0f;
+    vexp = kNoExp;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) acc[i] = (v4f)(0.0f);
+  }
+
+  __device__ __forceinline__ void lower(float by) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) acc[i] *= by;
+  }
+
+  // The weights of 32 tokens from tb on, as operand, with what the state needs before (Rows::settle).
+  __device__ __forceinline__ void weigh(v4f (&s)[2], const Scales& c, uint32_t tb, int lane,
+                                        h8 (&w)[PARTS]) {
+    if (tb + 32 > lim_lo) {
+      const uint32_t t = tb + 4 * (lane >> 4);
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[p][i] = t + 16 * p + i < lim ? s[p][i] : -INFINITY;
+    }
+    float f[2], top = -INFINITY;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      f[p] = fmaxf(qf * pow2i(c.ke[p]), FLT_MIN);
+      top = fmaxf(top, fmaxf(fmaxf(s[p][0], s[p][1]), fmaxf(s[p][2], s[p][3])) * f[p]);
+    }
+    if (__builtin_amdgcn_ballot_w64(top > m + (kLazy + kBias)) != 0) {
+      const float most = over_row<4>(top, [](float x, float y) { return fmaxf(x, y); });
+      const float mn = most > m + (kLazy + kBias) ? most - kBias : m;
+      const float down = __builtin_amdgcn_exp2f(m - mn);
+      l *= down;
+      lower(down);
+      m = mn;
+    }
+    const int vmax = max(c.ve[0], c.ve[1]);
+    if (vmax > vexp) {
+      lower(pow2i(vexp - vmax));
+      vexp = vmax;
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i], f[p], -m));
+        float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[p][i + 1], f[p], -m));
+        h2 v = cvt_h2(w0, w1);
+        if constexpr (PARTS == 1) {
+          l = __builtin_amdgcn_fdot2(v, (h2){(_Float16)1.0f, (_Float16)1.0f}, l, false);
+        } else {
+          l += w0 + w1;
+          const float down = pow2i(c.ve[p] - vexp);
+          w0 *= down, w1 *= down;
+          v = cvt_h2(w0, w1);
+          const h2 z = cvt_h2(w0 - (float)v.x, w1 - (float)v.y);
+          w[PARTS - 1][4 * p + i] = z.x, w[PARTS - 1][4 * p + i + 1] = z.y;
+        }
+        w[0][4 * p + i] = v.x, w[0][4 * p + i + 1] = v.y;
+      }
+    if constexpr (PARTS == 1)
+      if (__builtin_expect(min(c.ve[0], c.ve[1]) != vexp, 0)) {
+        const _Float16 d0 = (_Float16)pow2i(c.ve[0] - vexp), d1 = (_Float16)pow2i(c.ve[1] - vexp);
+        w[0] *= (h8){d0, d0, d0, d0, d1, d1, d1, d1};
+      }
+  }
+};
+
+// Up to 16 NR query rows per KV head: four waves, each on tokens of its own in a tile of 32 of its own,
+// which holds the keys and then, once the scores are there, the values.  No waits between the waves;
+// their sums meet in LDS at the end, and a row is finished by one wave.
+template <int D, int PARTS, int NR>
+__global__ __launch_bounds__(kBlockThreads, PARTS * NR == 1 ? 3 : PARTS * NR == 4 ? 1 : 2) void few_rows_kernel(RowsArgs a) {
+  using S = Shape<D, 4, PARTS>;
+  typedef float v4f __attribute__((ext_vector_type(4)));
+  constexpr int TILE = 32, NG = TILE / S::GROUP, PLANE = TILE * S::ROW, PITCH = D + 4;
+  constexpr int BYTES = PARTS * PLANE > 16 * PITCH * 4 ? PARTS * PLANE : (16 * PITCH * 4 + 1023) / 1024 * 1024;
+  __shared__ __attribute__((aligned(16))) char s_lut[2 * S::LUT];
+  __shared__ __attribute__((aligned(1024))) char s_wave[kWavesPerBlock][BYTES];
+  __shared__ float2 s_ml[kWavesPerBlock][16];
+  RowsWave<D, 4, PARTS> w(a);
+  if (!w.start()) return;
+  const uint32_t n_tiles = w.t1 - w.t0;
+  const uint32_t t0 = w.t0 + span_start(n_tiles, 4, w.wave), t1 = w.t0 + span_start(n_tiles, 4, w.wave + 1);
+  const int lane = w.lane, part = lane >> 4;
+  RawCodes raw[NG];                                      // the codes under way: keys, values, keys ...
+  auto load = [&](int kind, uint32_t t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g) raw[g] = w.load_group(kind, t * TILE + g * S::GROUP);
+  };
+  if (t0 < t1) {
+    if (a.pg.table) w.load_blocks((t0 * TILE) >> a.pg.block_log2);
+    load(0, t0);
+  }
+  w.load_tables(s_lut);
+  FewRows<D, PARTS> r[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) r[n].start(a, w.u, 16 * n, lane);
+  __syncthreads();                                       // the tables
+
+  char* const tile = s_wave[w.wave];
+  // (the swaps of tokens GROUP apart are the same)
+  auto rebuild_kind = [&](int kind, int (&e)[2]) __attribute__((always_inline)) {
+    const uint32_t t = (uint32_t)lane / S::LPV;
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+      e[g] = rebuild<D, PARTS>(raw[g], a.n[kind], a.log_norms[kind] != 0, s_lut + kind * S::LUT,
+                               tile + (t + g * S::GROUP) * S::ROW, PLANE, (uint32_t)lane % S::LPV,
+                               kind == 0 ? key_chunk<D>(0, t) : value_swap<D>(t));
+    if constexpr (NG == 1) e[1] = e[0];
+  };
+  // Chunk 4 k + part of the key of token lane % 16 lies at ka ^ 64 k, 16 tokens on 16 rows further;
+  // the lane's column piece of element block mb of values at va ^ 32 mb, likewise.
+  const uint32_t ka = (lane & 15) * S::ROW + 16u * key_chunk<D>(part, lane & 15);
+  const uint32_t tk = 4 * part + (((uint32_t)lane >> 2) & 3u);
+  const uint32_t va = tk * S::ROW + 16u * ((((uint32_t)lane >> 1) & 1u) ^ value_swap<D>(tk)) + 8u * (lane & 1);
+  for (uint32_t t = t0; t < t1; ++t) {
+    Scales c;
+    rebuild_kind(0, c.ke);
+    load(1, t);
+    wave_lds_sync();
+    v4f s[NR][2];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) s[n][0] = s[n][1] = (v4f)(0.0f);
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) {
+        const char* const at = tile + (ka ^ (64u * k)) + 16 * p * S::ROW;
+        const h8 h = read_h8(at);
+        h8 lo;
+        if constexpr (PARTS == 2) lo = read_h8(at + PLANE);
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          s[n][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h, r[n].q[0][k], s[n][p], 0, 0, 0);
+          if constexpr (PARTS == 2) {
+            s[n][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h, r[n].q[1][k], s[n][p], 0, 0, 0);
+            s[n][p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, r[n].q[0][k], s[n][p], 0, 0, 0);
+          }
+        }
+      }
+    wave_lds_sync();                                     // the keys are read
+    rebuild_kind(1, c.ve);
+    if (t + 1 < t1) load(0, t + 1);
+    h8 p[NR][PARTS];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) r[n].weigh(s[n], c, t * TILE, lane, p[n]);
+    wave_lds_sync();
+#pragma unroll
+    for (int mb = 0; mb < D / 16; ++mb) {
+      h8 v[PARTS];
+#pragma unroll
+      for (int z = 0; z < 2; ++z)
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) {
+          const s4 x = read_columns(tile + (va ^ (32u * mb)) + 16 * z * S::ROW + q * PLANE);
+          __builtin_memcpy((char*)&v[q] + 8 * z, &x, 8);
+        }
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        r[n].acc[mb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[0], p[n][0], r[n].acc[mb], 0, 0, 0);
+        if constexpr (PARTS == 2) {
+          r[n].acc[mb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[0], p[n][PARTS - 1], r[n].acc[mb], 0, 0, 0);
+          r[n].acc[mb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[PARTS - 1], p[n][0], r[n].acc[mb], 0, 0, 0);
+        }
+      }
+    }
+    wave_lds_sync();                                     // the values are read
+  }
+
+  // the waves' sums: row lane % 16, elements 16 mb + 4 part + i
+  constexpr int EPL = D / kWave;
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const bool none = r[n].m == kNoScore;
+    const float up = none ? 0.0f : pow2i(r[n].vexp);
+    const float sum = over_row<4>(r[n].l, [](float x, float y) { return x + y; });
+#pragma unroll
+    for (int mb = 0; mb < D / 16; ++mb) {
+      v4f x = r[n].acc[mb] * up;
+      if (none) x = (v4f)(0.0f);
+      *(v4f*)((float*)tile + (lane & 15) * PITCH + 16 * mb + 4 * part) = x;
+    }
+    if (lane < 16) s_ml[w.wave][lane] = make_float2(r[n].m, none ? 0.0f : sum);
+    __syncthreads();
+    for (uint32_t i = w.wave; i < 16; i += kWavesPerBlock) {
+      const uint32_t in_unit = 16 * n + i, row = w.u.rb * a.unit_rows + in_unit;
+      if (row >= w.u.rows) break;
+      float M = kNoScore, L = 0.0f, x[EPL];
+#pragma unroll
+      for (int v = 0; v < kWavesPerBlock; ++v) M = fmaxf(M, s_ml[v][i].x);
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) x[e] = 0.0f;
+#pragma unroll
+      for (int v = 0; v < kWavesPerBlock; ++v) {
+        const float2 ml = s_ml[v][i];
+        const float f = __builtin_amdgcn_exp2f(ml.x - M);
+        L = __builtin_fmaf(ml.y, f, L);
+#pragma unroll
+        for (int e = 0; e < EPL; ++e)
+          x[e] = __builtin_fmaf(((const float*)s_wave[v])[i * PITCH + EPL * lane + e], f, x[e]);
+      }
+      if (a.n_split == 1) {
+        const float inv = 1.0f / L;
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) x[e] = M == kNoScore ? 0.0f : x[e] * inv;
+        store_across<D>(a, w.u, row, x, lane);
+        continue;
+      }
+      const uint64_t at = ((uint64_t)w.unit * a.n_split + w.span) * a.unit_rows + in_unit;
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) a.ws_acc[at * D + EPL * lane + e] = x[e];
+      if (lane == 0) *(float2*)(a.ws_ml + at * 2) = make_float2(M, L);
+    }
+    if (n + 1 < NR) __syncthreads();
+  }
+}
+
 // The spans of one row, a row per wave, its elements across the lanes: M = max m, then
 // o = D W (sum 2^(m - M) acc) / (sum 2^(m - M) l).  The spans' (m, l) are read 64 at a time, one
 // per lane, and 8 spans' rows are requested together, the first ones before M is known.
@@ -904,7 +1183,6 @@ __global__ __launch_bounds__(kBlockThreads) void rows_merge_kernel(RowsArgs a) {
   };
   float2 v = load_ml(lane);
   load_acc(0);
-  const uint32_t smw = a.signs[(EPL * lane) / 2];
   float M = v.x;
   for (uint32_t s = (uint32_t)lane + kWave; s < spans; s += kWave) M = fmaxf(M, load_ml(s).x);
   M = wave_max(M);
@@ -930,18 +1208,7 @@ __global__ __launch_bounds__(kBlockThreads) void rows_merge_kernel(RowsArgs a) {
   const float inv = 1.0f / L;
 #pragma unroll
   for (int e = 0; e < EPL; ++e) x[e] = M == kNoScore ? 0.0f : x[e] * inv;
-  fwht_across_lanes<EPL>(x, lane);
-  apply_signs<EPL>(x, smw, lane);
-  const uint32_t j = row / a.G, g = row - j * a.G;
-  const uint64_t at = (uint64_t)u.b * a.o_stride[0] + (uint64_t)(u.h * a.G + g) * a.o_stride[1] +
-                      (uint64_t)j * a.o_stride[2] + EPL * lane;
-  if constexpr (EPL == 2) {
-    if (a.o_f32) *(float2*)((float*)a.o + at) = make_float2(x[0], x[1]);
-    else *(uint32_t*)((uint16_t*)a.o + at) = bf16x2_rne(x[0], x[1]);
-  } else {
-    if (a.o_f32) ((float*)a.o)[at] = x[0];
-    else ((uint16_t*)a.o)[at] = (uint16_t)(bf16x2_rne(x[0], 0.0f) & 0xFFFFu);
-  }
+  store_across<D>(a, u, row, x, lane);
 }
 
 template <int D>
@@ -952,9 +1219,12 @@ int launch(const RowsArgs& a, unsigned waves, bool wide, hipStream_t s) {
     hipLaunchKernelGGL((rows_tiles_kernel<D>), dim3(a.B * a.H * a.n_tiles), dim3(4 * kWave), 0, s, a);
     if (hipGetLastError() != hipSuccess) return -2;
   }
-  if (waves == 1) {
-    if (wide) hipLaunchKernelGGL((rows_kernel<D, 1, 2>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((rows_kernel<D, 1, 1>), grid, block, 0, s, a);
+  if (a.unit_rows == 16) {
+    if (wide) hipLaunchKernelGGL((few_rows_kernel<D, 2, 1>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((few_rows_kernel<D, 1, 1>), grid, block, 0, s, a);
+  } else if (a.unit_rows == 32) {
+    if (wide) hipLaunchKernelGGL((few_rows_kernel<D, 2, 2>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((few_rows_kernel<D, 1, 2>), grid, block, 0, s, a);
   } else if (waves == 8) {
     if (wide) hipLaunchKernelGGL((rows_kernel<D, 8, 2>), grid, block, 0, s, a);
     else if (a.ws_tiles) hipLaunchKernelGGL((rows_many_kernel<D>), grid, block, 0, s, a);
