@@ -927,13 +927,9 @@ struct FewRows {
 
   __device__ __forceinline__ void start(const RowsArgs& a, const Unit& u, uint32_t first, int lane) {
     const uint32_t r = min(u.rb * a.unit_rows + first + (lane & 15), u.rows - 1);
-    const uint32_t j = r / a.G, g = r - j * a.G;
-    const int64_t seen = u.pos0 + j + 1;
+    const int64_t seen = u.pos0 + r / a.G + 1;
     lim = seen < 0 ? 0u : (uint32_t)seen;
     lim_lo = (uint32_t)__builtin_amdgcn_readlane((int)lim, 0);
-    const uint64_t at = (uint64_t)u.b * a.q_stride[0] + (uint64_t)(u.h * a.G + g) * a.q_stride[1] +
-                        (uint64_t)j * a.q_stride[2];
-    qf = load_rows<D, PARTS, 4>(a, at, lane, q);
     m = kNoScore;
     l = 0.0f;
     vexp = kNoExp;
@@ -1002,6 +998,51 @@ struct FewRows {
   }
 };
 
+// A query row on 16 lanes, d / 16 elements each: four rows a wave.  As requested, and transformed.
+template <int D>
+struct QueryPiece {
+  static constexpr int N = D / 16;
+  uint32_t raw[N], signs[N / 2];
+
+  __device__ __forceinline__ void request(const RowsArgs& a, const Unit& u, uint32_t row, int lane) {
+    const uint32_t r = min(row, u.rows - 1), j = r / a.G, g = r - j * a.G;
+    const uint32_t e = N * (lane & 15);
+    const uint64_t at = (uint64_t)u.b * a.q_stride[0] + (uint64_t)(u.h * a.G + g) * a.q_stride[1] +
+                        (uint64_t)j * a.q_stride[2] + e;
+    load_words<N / 2>(a.signs + e / 2, signs);
+    if (a.q_f32) load_words<N>((const uint32_t*)a.q + at, raw);
+    else load_words<N / 2>((const uint32_t*)((const uint16_t*)a.q + at), raw);
+  }
+
+  // scale W D q, scaled so that the largest element of the row is in [2^7, 2^8), into x; the exponent
+  // taken out.
+  __device__ __forceinline__ int transform(const RowsArgs& a, int lane, float (&x)[N]) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t v = a.q_f32 ? raw[i] : i % 2 ? raw[i / 2] & 0xFFFF0000u : raw[i / 2] << 16;
+      x[i] = __uint_as_float(v ^ ((i % 2 ? signs[i / 2] : signs[i / 2] << 16) & 0x80000000u));
+    }
+#pragma unroll
+    for (int h = 1; h < N; h <<= 1) stage_regs(x, h);
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i] = fwht_stage<8>(fwht_stage<4>(fwht_stage<2>(fwht_stage<1>(x[i], lane), lane), lane), lane);
+      x[i] *= a.qscale;
+      top = fmaxf(top, fabsf(x[i]));
+    }
+    top = fmaxf(top, row_ror<8>(top));
+    top = fmaxf(top, row_ror<4>(top));
+    top = fmaxf(top, row_ror<2>(top));
+    top = fmaxf(top, row_ror<1>(top));
+    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127 - 7, -119), 120);
+    const float down = pow2i(-e);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] *= down;
+    return e;
+  }
+};
+
 // Up to 16 NR query rows per KV head: four waves, each on tokens of its own in a tile of 32 of its own,
 // which holds the keys and then, once the scores are there, the values.  No waits between the waves;
 // their sums meet in LDS at the end, and a row is finished by one wave.
@@ -1024,15 +1065,63 @@ __global__ __launch_bounds__(kBlockThreads, PARTS * NR == 1 ? 3 : PARTS * NR == 
 #pragma unroll
     for (int g = 0; g < NG; ++g) raw[g] = w.load_group(kind, t * TILE + g * S::GROUP);
   };
+  // Everything the start needs is requested before any of it is used: a table entry a thread, 4 NR
+  // query rows a wave, the first codes.
+  float2 entry[2];
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind)
+    entry[kind] = ((const float2*)a.lut[kind])[min(threadIdx.x, a.n[kind] - 1)];
+  QueryPiece<D> piece[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n)
+    piece[n].request(a, w.u, w.u.rb * a.unit_rows + 16 * n + 4 * w.wave + part, lane);
   if (t0 < t1) {
     if (a.pg.table) w.load_blocks((t0 * TILE) >> a.pg.block_log2);
     load(0, t0);
   }
-  w.load_tables(s_lut);
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    char* const at = s_lut + kind * S::LUT;
+    if constexpr (PARTS == 1) ((h2*)at)[threadIdx.x] = cvt_h2(entry[kind].x, entry[kind].y);
+    else ((float2*)at)[threadIdx.x] = entry[kind];
+  }
+  // q^ of all rows by way of LDS (where the tiles will be), chunks in the places of a tile of keys
+  char* const s_q = s_wave[0];
+  constexpr int Q_PLANE = 16 * NR * S::ROW;
+  static_assert(PARTS * Q_PLANE <= kWavesPerBlock * BYTES, "q^ fits the tiles' places");
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    constexpr int N = D / 16;
+    float x[N];
+    const int e = piece[n].transform(a, lane, x);
+    const uint32_t i = 4 * w.wave + part, at = N * (lane & 15) * 2;          // row of the 16, byte in it
+    char* const dst = s_q + (16 * n + i) * S::ROW + 16u * key_chunk<D>(at / 16, i) + at % 16;
+    uint32_t hi[N / 2], lo[N / 2];
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) {
+      const h2 h = cvt_h2(x[2 * k], x[2 * k + 1]);
+      hi[k] = h2_bits(h);
+      lo[k] = h2_bits(cvt_h2(x[2 * k] - (float)h.x, x[2 * k + 1] - (float)h.y));
+    }
+    store_words<N / 2>((uint32_t*)dst, hi);
+    if constexpr (PARTS == 2) store_words<N / 2>((uint32_t*)(dst + Q_PLANE), lo);
+    if ((lane & 15) == 0) s_ml[n][i].x = pow2i(e);
+  }
+  static_assert(NR <= kWavesPerBlock, "a factor per row");
+  __syncthreads();
   FewRows<D, PARTS> r[NR];
 #pragma unroll
-  for (int n = 0; n < NR; ++n) r[n].start(a, w.u, 16 * n, lane);
-  __syncthreads();                                       // the tables
+  for (int n = 0; n < NR; ++n) {
+    r[n].start(a, w.u, 16 * n, lane);
+    r[n].qf = s_ml[n][lane & 15].x;
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+      for (int q = 0; q < PARTS; ++q)
+        r[n].q[q][k] = read_h8(s_q + q * Q_PLANE + (16 * n + (lane & 15)) * S::ROW +
+                               16u * key_chunk<D>(4 * k + part, lane & 15));
+  }
+  __syncthreads();                                       // q^ is read, the tables are there
 
   char* const tile = s_wave[w.wave];
   // (the swaps of tokens GROUP apart are the same)
