@@ -163,6 +163,11 @@ __device__ __forceinline__ uint32_t score_key(float s) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
+// Set bits of a ballot below the lane's own.
+__device__ __forceinline__ uint32_t lanes_below(uint64_t m) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+
 // A fp64 value of lane ^ B.
 template <int B>
 __device__ __forceinline__ double lane_xor_f64(double v) {
@@ -259,9 +264,12 @@ __global__ __launch_bounds__(kBlockThreads) void block_score_kernel(SelectArgs a
 // The n_sel largest keys of one (sequence, KV head), the lower block first among equals; the first
 // and last blocks stand outside the comparison.  With x = key - smallest key, the x of the last
 // kept block is found from its top down, 8 bits a step, by counting the x that share the bits found
-// so far (most steps end early: as soon as all of a bin are kept); then every thread counts the
-// kept among its KPT consecutive keys, and one scan gives their places.  KPT = 0: keys are read
-// again in every step, a thread's share of any length.
+// so far (most steps end early: as soon as all of a bin are kept).  Counting is what takes the time,
+// as keys next to each other in value fall on one counter.  So with more than 4 keys a thread and no
+// more blocks to keep than threads, the same is done first for the largest key of each thread: at
+// least `want` keys are not below the want-th of those, and only they are counted.
+// A wave looks after KPT x 64 consecutive keys (KPT = 0: of any number, read again in every step),
+// 64 at a time in ascending order, so that places among the kept come from counted ballots.
 template <int THREADS, int KPT>
 __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
   constexpr uint32_t WAVES = THREADS / kWave;
@@ -288,24 +296,65 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
   if (want == 0) return;
   const uint32_t* const keys = a.keys + (uint64_t)row * a.n_keys + a.n_first;
   const uint32_t per = KPT > 0 ? (uint32_t)KPT : (m + THREADS - 1) / THREADS;
-  const uint32_t first = min(t * per, m), mine = min(per, m - first);
+  const uint32_t first = wave * per * kWave + lane;
   uint32_t k[KPT > 0 ? KPT : 1];
   if constexpr (KPT > 0) {
 #pragma unroll
-    for (int c = 0; c < KPT; ++c) k[c] = keys[min(first + c, m - 1)];
+    for (int c = 0; c < KPT; ++c) k[c] = keys[min(first + c * kWave, m - 1)];
   }
-  // f(x's place, x) for each of the thread's keys
+  // f(place, key, whether there is one) for the thread's keys, by all threads
   auto each = [&](auto&& f) {
     if constexpr (KPT > 0) {
 #pragma unroll
-      for (int c = 0; c < KPT; ++c)
-        if ((uint32_t)c < mine) f(first + c, k[c]);
+      for (int c = 0; c < KPT; ++c) f(first + c * kWave, k[c], first + c * kWave < m);
     } else {
-      for (uint32_t c = 0; c < mine; ++c) f(first + c, keys[first + c]);
+      for (uint32_t c = 0, i = first; c < per; ++c, i += kWave) f(i, keys[min(i, m - 1)], i < m);
     }
   };
-  uint32_t low = 0xFFFFFFFFu, top = 0;
-  each([&](uint32_t, uint32_t x) { low = min(low, x), top = max(top, x); });
+  uint32_t left;                                   // bits of x = key - low yet to find
+  uint32_t need = want;                            // kept among those that share the bits found
+  // The bits found of the need-th largest x among those that `visit` hands out, in `steps` steps.
+  auto find = [&](auto&& visit, uint32_t low, uint32_t steps) {
+    uint32_t found = 0;
+    for (; left > 0 && steps > 0; --steps) {
+      const uint32_t w = min(left, 8u), sh = left - w;
+      __syncthreads();                             // s_wave and s_pick are read
+      for (uint32_t i = t; i < 256; i += THREADS) s_hist[i] = 0;
+      __syncthreads();
+      visit([&](uint32_t, uint32_t x, bool there) {
+        const uint64_t v = x - low;
+        if (there && x >= low && (v >> left) == found)
+          atomicAdd(&s_hist[(uint32_t)(v >> sh) & ((1u << w) - 1u)], 1u);
+      });
+      __syncthreads();
+      if (wave == 0) {                             // lane l: bins 255 - 4 l down to 252 - 4 l
+        const uint4 v = *(const uint4*)(s_hist + 252 - 4 * lane);
+        const uint32_t sum = v.x + v.y + v.z + v.w;
+        const uint32_t end = wave_scan(sum);
+        uint32_t before = end - sum;
+        if (before < need && end >= need) {
+          const uint32_t c[4] = {v.w, v.z, v.y, v.x};
+          uint32_t i = 0;
+          while (before + c[i] < need) before += c[i++];
+          s_pick[0] = 255 - 4 * lane - i, s_pick[1] = before, s_pick[2] = c[i];
+        }
+      }
+      __syncthreads();
+      found = (found << w) | s_pick[0];
+      need -= s_pick[1];
+      left = sh;
+      if (s_pick[2] == need) break;                // all of the bin are kept
+    }
+    return found;
+  };
+  const uint32_t share = per * kWave;
+  const uint32_t threads = m / share * kWave + min(m % share, (uint32_t)kWave);    // with keys
+  const bool prune = KPT != 4 && want <= threads;
+  uint32_t least = 0xFFFFFFFFu, most = 0;
+  each([&](uint32_t, uint32_t x, bool there) {
+    if (there) least = min(least, x), most = max(most, x);
+  });
+  uint32_t low = prune && first < m ? most : least, top = most;
 #pragma unroll
   for (int s = 1; s < kWave; s <<= 1) {
     low = min(low, (uint32_t)__shfl_xor((int)low, s));
@@ -314,54 +363,35 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
   if (lane == 0) s_wave[0][wave] = low, s_wave[1][wave] = top;
   __syncthreads();
   for (uint32_t w = 0; w < WAVES; ++w) low = min(low, s_wave[0][w]), top = max(top, s_wave[1][w]);
-  uint32_t left = top == low ? 0u : 32u - (uint32_t)__builtin_clz(top - low);   // bits of x to find
-  uint32_t found = 0, need = want;                 // bits found; kept among those that share them
-  while (left > 0) {
-    const uint32_t w = min(left, 8u), sh = left - w;
-    __syncthreads();                               // s_wave and s_pick are read
-    for (uint32_t i = t; i < 256; i += THREADS) s_hist[i] = 0;
-    __syncthreads();
-    each([&](uint32_t, uint32_t x) {
-      const uint64_t v = x - low;
-      if ((v >> left) == found) atomicAdd(&s_hist[(uint32_t)(v >> sh) & ((1u << w) - 1u)], 1u);
-    });
-    __syncthreads();
-    if (wave == 0) {                               // lane l: bins 255 - 4 l down to 252 - 4 l
-      const uint4 v = *(const uint4*)(s_hist + 252 - 4 * lane);
-      const uint32_t sum = v.x + v.y + v.z + v.w;
-      const uint32_t end = wave_scan(sum);
-      uint32_t before = end - sum;
-      if (before < need && end >= need) {
-        const uint32_t c[4] = {v.w, v.z, v.y, v.x};
-        uint32_t i = 0;
-        while (before + c[i] < need) before += c[i++];
-        s_pick[0] = 255 - 4 * lane - i, s_pick[1] = before, s_pick[2] = c[i];
-      }
-    }
-    __syncthreads();
-    found = (found << w) | s_pick[0];
-    need -= s_pick[1];
-    left = sh;
-    if (s_pick[2] == need) break;                  // all of the bin are kept
+  auto bits = [&]() { return top == low ? 0u : 32u - (uint32_t)__builtin_clz(top - low); };
+  left = bits();
+  if (prune) {
+    const uint32_t found = find([&](auto&& f) { f(first, most, first < m); }, low, 2);
+    low += found << left;
+    left = bits();
+    need = want;
   }
+  const uint32_t found = find(each, low, 4);
   // kept: x >> left above `found`, and the first `need` that equal it
-  uint32_t above = 0, equal = 0;
-  each([&](uint32_t, uint32_t x) {
-    const uint32_t v = (uint32_t)((uint64_t)(x - low) >> left);
-    above += v > found ? 1u : 0u;
-    equal += v == found ? 1u : 0u;
+  auto above = [&](uint32_t x, bool there) { return there && x >= low && (x - low) >> left > found; };
+  auto equal = [&](uint32_t x, bool there) { return there && x >= low && (x - low) >> left == found; };
+  uint32_t na = 0, ne = 0;
+  each([&](uint32_t, uint32_t x, bool there) {
+    na += __popcll(__builtin_amdgcn_ballot_w64(above(x, there)));
+    ne += __popcll(__builtin_amdgcn_ballot_w64(equal(x, there)));
   });
-  uint32_t ea = wave_scan(above), ee = wave_scan(equal);
   __syncthreads();
-  if (lane == kWave - 1) s_wave[0][wave] = ea, s_wave[1][wave] = ee;
+  if (lane == 0) s_wave[0][wave] = na, s_wave[1][wave] = ne;
   __syncthreads();
-  ea -= above, ee -= equal;
-  for (uint32_t w = 0; w < wave; ++w) ea += s_wave[0][w], ee += s_wave[1][w];
-  each([&](uint32_t i, uint32_t x) {
-    const uint32_t v = (uint32_t)((uint64_t)(x - low) >> left);
-    if (v > found || (v == found && ee < need)) out[a.n_first + ea + min(ee, need)] = (int32_t)(a.n_first + i);
-    ea += v > found ? 1u : 0u;
-    ee += v == found ? 1u : 0u;
+  na = ne = 0;
+  for (uint32_t w = 0; w < wave; ++w) na += s_wave[0][w], ne += s_wave[1][w];
+  each([&](uint32_t i, uint32_t x, bool there) {
+    const bool is_above = above(x, there), is_equal = equal(x, there);
+    const uint64_t ma = __builtin_amdgcn_ballot_w64(is_above), me = __builtin_amdgcn_ballot_w64(is_equal);
+    const uint32_t ea = na + lanes_below(ma), ee = ne + lanes_below(me);
+    if (is_above || (is_equal && ee < need)) out[a.n_first + ea + min(ee, need)] = (int32_t)(a.n_first + i);
+    na += __popcll(ma);
+    ne += __popcll(me);
   });
 }
 

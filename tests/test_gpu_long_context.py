@@ -418,6 +418,9 @@ SELECT = [
     (128, 1, 64, 32, 40, 1280, [1279], 39, 0, 1),
     (64, 1, 5, 128, 20, 2560, [2433, 1], 1, 0, 1),
     (64, 2, 16, 32, 1100, 35200, [35200, 31], 1024, 0, 1),
+    (64, 1, 4, 32, 3001, 96032, [96032, 3300, 40000], 70, 3, 7),       # few of many
+    (64, 1, 2, 32, 17003, 544096, [544096, 530000, 7000, 50000], 201, 0, 1),
+    (64, 1, 1, 32, 16600, 531200, [531200], 1300, 5, 9),
 ]
 
 
