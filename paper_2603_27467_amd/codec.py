@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes
+import functools
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
@@ -31,10 +32,10 @@ def _stream_handle(stream) -> int:
 
 def desc_of(t, layers: Optional[int] = None) -> C.tvq_tensor_desc:
     """Descriptor of a [L, B, H, T, d] torch tensor (d contiguous)."""
-    if t.dim() != 5 or t.stride(-1) != 1:
+    shape, s = t.shape, t.stride()
+    if len(shape) != 5 or s[4] != 1:
         raise ValueError("expected a [L, B, H, T, d] tensor with d contiguous")
-    s = t.stride()
-    return C.tvq_tensor_desc(t.shape[1], t.shape[3], s[0], s[1], s[2], s[3])
+    return C.tvq_tensor_desc(shape[1], shape[3], s[0], s[1], s[2], s[3])
 
 
 def _check_bytes(buf, lay: C.tvq_layout, what: str) -> None:
@@ -48,8 +49,15 @@ def _check_bytes(buf, lay: C.tvq_layout, what: str) -> None:
 
 
 def _on_gpu(*tensors) -> None:
-    if not all(t.is_cuda for t in tensors):
-        raise ValueError("tensors must be on the GPU")
+    for t in tensors:
+        if not t.is_cuda:
+            raise ValueError("tensors must be on the GPU")
+
+
+@functools.lru_cache(maxsize=None)
+def _dtypes() -> dict:
+    import torch
+    return {torch.bfloat16: C.TVQ_BF16, torch.float32: C.TVQ_F32}
 
 
 class Codec:
@@ -87,18 +95,19 @@ class Codec:
     def _check_kv(self, t, what: str) -> None:
         """t must be a [L, B, H, T, d] GPU tensor of this codec's L, H and d (the kernels take
         L, H and d from the codec, so a smaller tensor would be read or written past its end)."""
-        if t.dim() != 5:
+        s = t.shape
+        if len(s) != 5:
             raise ValueError(f"{what} must be a [L, B, H, T, d] GPU tensor")
-        if t.shape[0] != self.L or t.shape[2] != self.H or t.shape[4] != self.d:
-            raise ValueError(f"{what} has shape {tuple(t.shape)}; the codec needs "
+        if s[0] != self.L or s[2] != self.H or s[4] != self.d:
+            raise ValueError(f"{what} has shape {tuple(s)}; the codec needs "
                              f"[{self.L}, B, {self.H}, T, {self.d}]")
 
     def _check_q(self, q, out) -> None:
-        if q.dim() != 3 or out.shape != q.shape or not q.is_contiguous() or \
-                not out.is_contiguous():
+        s = q.shape
+        if len(s) != 3 or out.shape != s or not q.is_contiguous() or not out.is_contiguous():
             raise ValueError("q and out must be contiguous [B, Hq, d] GPU tensors")
-        if q.shape[2] != self.d:
-            raise ValueError(f"q has head dim {q.shape[2]}, the codec {self.d}")
+        if s[2] != self.d:
+            raise ValueError(f"q has head dim {s[2]}, the codec {self.d}")
 
     def layout(self, batch: int, capacity_tokens: int) -> C.tvq_layout:
         return C.tvq_cache_layout(self.handle, batch, capacity_tokens)
@@ -277,18 +286,19 @@ class Codec:
         return C.tvq_attention_prefill_workspace(self.handle, batch, num_q_heads, tokens, max_ctx)
 
     def _check_rows(self, q, out) -> None:
-        if q.dim() != 4 or out.shape != q.shape or q.stride(-1) != 1 or out.stride(-1) != 1:
+        s = q.shape
+        if len(s) != 4 or out.shape != s or q.stride(-1) != 1 or out.stride(-1) != 1:
             raise ValueError("q and out must be [B, Hq, T, d] GPU tensors with d contiguous")
-        if q.shape[3] != self.d:
-            raise ValueError(f"q has head dim {q.shape[3]}, the codec {self.d}")
+        if s[3] != self.d:
+            raise ValueError(f"q has head dim {s[3]}, the codec {self.d}")
 
     @staticmethod
     def _io_dtypes(q, out):
-        import torch
-        dts = {torch.bfloat16: C.TVQ_BF16, torch.float32: C.TVQ_F32}
-        if q.dtype not in dts or out.dtype not in dts:
+        dts = _dtypes()
+        dq, do = dts.get(q.dtype), dts.get(out.dtype)
+        if dq is None or do is None:
             raise ValueError("q/out must be bf16 or fp32")
-        return dts[q.dtype], dts[out.dtype]
+        return dq, do
 
     @staticmethod
     def _rows_desc(t) -> C.tvq_tensor_desc:
@@ -357,27 +367,25 @@ class Codec:
     def _check_bounds(self, bounds, pool_lay: C.tvq_layout) -> None:
         import torch
         want = (self.L, pool_lay.batch, self.H, 2, self.d)
-        if bounds.dtype != torch.bfloat16 or not bounds.is_contiguous() or \
-                tuple(bounds.shape) != want:
+        if bounds.dtype != torch.bfloat16 or bounds.shape != want or not bounds.is_contiguous():
             raise ValueError(f"bounds must be a contiguous bf16 GPU tensor of shape {want}")
 
     def key_bounds_paged(self, k, positions, block_table, bounds, pool_lay: C.tvq_layout,
                          stream=None) -> None:
         """Bring the key bounds of the pool's blocks up to date with the keys of an encode_paged
         call (the same k, positions and block_table)."""
-        import torch
-        dt = {torch.bfloat16: C.TVQ_BF16, torch.float32: C.TVQ_F32}.get(k.dtype)
+        dt = _dtypes().get(k.dtype)
         if dt is None:
             raise ValueError("k must be bf16 or fp32")
         self._check_kv(k, "k")
         self._check_bounds(bounds, pool_lay)
         _on_gpu(k, bounds)
-        if block_table.dim() != 2 or positions.shape != (k.shape[1],) or \
-                block_table.shape[0] != k.shape[1]:
+        desc, table = desc_of(k), block_table.shape
+        if len(table) != 2 or table[0] != desc.batch or positions.shape != (desc.batch,):
             raise ValueError("positions [B] and block_table [B, max_blocks] must match k")
-        C.tvq_key_bounds_paged(self.handle, dt, k.data_ptr(), desc_of(k),
+        C.tvq_key_bounds_paged(self.handle, dt, k.data_ptr(), desc,
                                self._i32(positions, "positions"),
-                               self._i32(block_table, "block_table"), block_table.shape[1],
+                               self._i32(block_table, "block_table"), table[1],
                                bounds.data_ptr(), pool_lay, _stream_handle(stream))
 
     def select_blocks_workspace_bytes(self, batch: int, max_ctx: int, block_tokens: int) -> int:
@@ -389,26 +397,26 @@ class Codec:
         """For q ([B, Hq, d]) and each KV head, the blocks of the context whose keys can score
         highest, into blocks ([B, H, n_sel] int32, ascending, -1 behind them) and their tokens into
         sel_lens ([B, H] int32).  The first n_first and last n_last blocks are always among them."""
-        import torch
-        if q.dim() != 3 or not q.is_contiguous() or q.shape[2] != self.d:
+        shape, table, lists = q.shape, block_table.shape, blocks.shape
+        if len(shape) != 3 or shape[2] != self.d or not q.is_contiguous():
             raise ValueError(f"q must be a contiguous [B, Hq, {self.d}] GPU tensor")
         self._check_bounds(bounds, pool_lay)
         _on_gpu(q, bounds, block_table, ctx_lens, blocks, sel_lens)
-        dt = {torch.bfloat16: C.TVQ_BF16, torch.float32: C.TVQ_F32}.get(q.dtype)
+        dt = _dtypes().get(q.dtype)
         if dt is None:
             raise ValueError("q must be bf16 or fp32")
-        B = q.shape[0]
-        if block_table.dim() != 2 or block_table.shape[0] != B or ctx_lens.shape != (B,):
+        B, Hq, _ = shape
+        if len(table) != 2 or table[0] != B or ctx_lens.shape != (B,):
             raise ValueError("block_table [B, max_blocks] and ctx_lens [B] must match q")
-        if blocks.dim() != 3 or blocks.shape[:2] != (B, self.H) or sel_lens.shape != (B, self.H):
+        if len(lists) != 3 or lists[0] != B or lists[1] != self.H or sel_lens.shape != lists[:2]:
             raise ValueError("blocks [B, H, n_sel] and sel_lens [B, H] must match q and the codec")
         workspace = self._workspace(
             workspace, lambda: self.select_blocks_workspace_bytes(B, max_ctx,
                                                                   pool_lay.capacity_tokens), q.device)
         C.tvq_select_blocks(self.handle, bounds.data_ptr(), pool_lay,
-                            self._i32(block_table, "block_table"), block_table.shape[1],
-                            self._i32(ctx_lens, "ctx_lens"), max_ctx, B, layer, q.shape[1], dt,
-                            q.data_ptr(), blocks.shape[2], n_first, n_last,
+                            self._i32(block_table, "block_table"), table[1],
+                            self._i32(ctx_lens, "ctx_lens"), max_ctx, B, layer, Hq, dt,
+                            q.data_ptr(), lists[2], n_first, n_last,
                             self._i32(blocks, "blocks"), self._i32(sel_lens, "sel_lens"),
                             workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
 
@@ -425,18 +433,18 @@ class Codec:
         _check_bytes(pool, pool_lay, "pool")
         _on_gpu(q, out, pool, block_table, blocks, sel_lens)
         dq, do = self._io_dtypes(q, out)
-        B, Hq, _ = q.shape
-        if block_table.dim() != 2 or block_table.shape[0] != B:
+        (B, Hq, _), table, lists = q.shape, block_table.shape, blocks.shape
+        if len(table) != 2 or table[0] != B:
             raise ValueError("block_table [B, max_blocks] must match q")
-        if blocks.dim() != 3 or blocks.shape[:2] != (B, self.H) or sel_lens.shape != (B, self.H):
+        if len(lists) != 3 or lists[0] != B or lists[1] != self.H or sel_lens.shape != lists[:2]:
             raise ValueError("blocks [B, H, n_sel] and sel_lens [B, H] must match q and the codec")
-        n_sel = blocks.shape[2]
+        n_sel = lists[2]
         workspace = self._workspace(
             workspace, lambda: self.attention_blocks_workspace_bytes(B, Hq, n_sel,
                                                                      pool_lay.capacity_tokens),
             q.device)
         C.tvq_attention_blocks(self.handle, pool.data_ptr(), pool_lay,
-                               self._i32(block_table, "block_table"), block_table.shape[1],
+                               self._i32(block_table, "block_table"), table[1],
                                self._i32(blocks, "blocks"), n_sel, self._i32(sel_lens, "sel_lens"),
                                B, layer, Hq, scale, dq, q.data_ptr(), do, out.data_ptr(),
                                workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
