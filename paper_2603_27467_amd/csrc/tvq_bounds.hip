@@ -68,16 +68,28 @@ __device__ __forceinline__ void add_key(Bounds8& m, const void* k, uint64_t elem
   }
 }
 
+// f over the values of the lanes that hold the same channels: a value every LPT lanes.
+template <int LPT, class F>
+__device__ __forceinline__ float over_tokens(float x, F f) {
+  if constexpr (LPT == 8) x = f(x, row_ror<8>(x));
+  uint32_t u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  u = __float_as_uint(f(__uint_as_float(r[0]), __uint_as_float(r[1])));
+  const auto h = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return f(__uint_as_float(h[0]), __uint_as_float(h[1]));
+}
+
 // The tokens of a call that fall into one pool block of one (layer, sequence, KV head): d / 8 lanes
 // hold the channels of a token, 8 a lane (16 bytes of bf16).  SLOTS groups of such lanes share the
-// tokens of a block and are summed up in LDS; the order of blocks follows the heads, which a
-// projection leaves beside each other in memory and which the bounds hold beside each other too.
+// tokens of a block: one where a block gets few tokens, a wave else.  The order of blocks follows the
+// heads, which a projection leaves beside each other in memory and which the bounds hold beside each
+// other too.
 template <int D, bool F32, int SLOTS>
 __global__ __launch_bounds__(kBlockThreads) void key_bounds_kernel(KeyBoundsArgs a) {
   constexpr int LPT = D / 8;                       // lanes of a token
   constexpr int GROUPS = kBlockThreads / LPT;      // of a workgroup
   constexpr int TASKS = GROUPS / SLOTS;            // blocks of a workgroup
-  static_assert(SLOTS == 1 || SLOTS == GROUPS, "a group or a workgroup per block");
+  static_assert(SLOTS == 1 || SLOTS == kWave / LPT, "a group or a wave per block");
   const uint32_t sub = threadIdx.x % LPT, group = threadIdx.x / LPT;
   const uint32_t slot = group % SLOTS;
   const uint64_t task = (uint64_t)blockIdx.x * TASKS + group / SLOTS;
@@ -111,17 +123,12 @@ __global__ __launch_bounds__(kBlockThreads) void key_bounds_kernel(KeyBoundsArgs
       add_key<F32>(m, a.k, base + (uint64_t)(t0 + t) * a.stride_t);
   }
   if constexpr (SLOTS > 1) {
-    __shared__ float s_lo[SLOTS][D + 4], s_hi[SLOTS][D + 4];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) s_lo[slot][8 * sub + c] = m.lo[c], s_hi[slot][8 * sub + c] = m.hi[c];
-    __syncthreads();
+    for (int c = 0; c < 8; ++c) {
+      m.lo[c] = over_tokens<LPT>(m.lo[c], [](float x, float y) { return fminf(x, y); });
+      m.hi[c] = over_tokens<LPT>(m.hi[c], [](float x, float y) { return fmaxf(x, y); });
+    }
     if (slot != 0) return;
-    for (int s = 1; s < SLOTS; ++s)
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        m.lo[c] = fminf(m.lo[c], s_lo[s][8 * sub + c]);
-        m.hi[c] = fmaxf(m.hi[c], s_hi[s][8 * sub + c]);
-      }
   }
   if (!work) return;
   uint16_t* out = a.bounds + ((((uint64_t)l * a.pg.n_blocks + blk) * a.H + h) * 2) * D + 8 * sub;
@@ -395,13 +402,19 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
   });
 }
 
+// Tokens of a block up to which a group takes it.  32 layers, 16 sequences, 8 heads of d = 128, us by
+// a group and by a wave: 1 token 4.8 and 6.4, 8 tokens 5.2 and 11.5, 16 tokens 7.2 and 11.2; 4,099
+// tokens of one sequence 58 and 53, of which the copy rate of the device (5.15 TB/s) would need 54.
+constexpr uint32_t kGroupTokens = 16;
+
 template <int D, bool F32>
 void launch_bounds(const KeyBoundsArgs& a, hipStream_t s) {
   constexpr uint32_t GROUPS = kBlockThreads / (D / 8);
   const uint64_t tasks = (uint64_t)a.L * a.B * a.n_touch * a.H;
   const uint64_t per = (uint64_t)min(a.T, 1u << a.pg.block_log2);    // tokens of a block at most
-  if (per > 4)
-    hipLaunchKernelGGL((key_bounds_kernel<D, F32, GROUPS>), dim3((unsigned)tasks),
+  if (per > kGroupTokens)
+    hipLaunchKernelGGL((key_bounds_kernel<D, F32, kWave / (D / 8)>),
+                       dim3((unsigned)((tasks + kWavesPerBlock - 1) / kWavesPerBlock)),
                        dim3(kBlockThreads), 0, s, a);
   else
     hipLaunchKernelGGL((key_bounds_kernel<D, F32, 1>), dim3((unsigned)((tasks + GROUPS - 1) / GROUPS)),

@@ -103,13 +103,15 @@ inline RowsPlan rows_plan(int64_t batch, int64_t heads, int64_t rows, int64_t to
   const int64_t tiles = ceil_div(tokens, p.tile);
   const int64_t fill = 4 * places / p.units + 1;      // past four rounds of places nothing is gained
   const int64_t most = tokens / (p.min_tiles * (int64_t)p.tile);
-  const auto time = [&](int64_t n) {
-    return ceil_div(p.units * n, places) *
-           (ceil_div(tiles, few ? 4 * n : n) + (n > 1 ? kSpanTiles : 0));
-  };
-  int64_t best = 1;
-  for (int64_t n = 2; n <= most && n <= fill; ++n)
-    if (time(n) < time(best)) best = n;
+  const int64_t lanes = few ? 4 : 1;                  // waves that share a span's tiles among them
+  int64_t best = 1, least = ceil_div(p.units, places) * ceil_div(tiles, lanes);
+  for (int64_t n = 2; n <= most && n <= fill;) {
+    const int64_t per = ceil_div(tiles, lanes * n);
+    const int64_t time = ceil_div(p.units * n, places) * (per + kSpanTiles);
+    if (time < least) best = n, least = time;
+    if (per == 1) break;
+    n = ceil_div(tiles, lanes * (per - 1));           // more spans of as many tiles save nothing
+  }
   p.n_split = (uint32_t)best;
   const int64_t parts = p.n_split > 1 ? p.units * p.n_split * p.unit_rows : 0;
   p.acc_bytes = (parts * d * 4 + 255) / 256 * 256;

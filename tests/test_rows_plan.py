@@ -89,6 +89,21 @@ def test_plans(rows):
             (4, 32, True, False), (4, 32, False, False)} <= seen
 
 
+def test_the_number_of_spans_takes_the_least_time(rows):
+    """Against the rule over every number: rounds of the device's places, times the tiles of a span
+    and three more where there are several."""
+    rng = np.random.default_rng(3)
+    for _ in range(400):
+        lines, n_rows = int(math.exp(rng.uniform(0, 5))), int(math.exp(rng.uniform(0, 8)))
+        tokens = int(math.exp(rng.uniform(3, 12)))
+        p = rows.plan(lines, 1, n_rows, tokens, 128, 256)
+        places = 256 if p["waves"] == 8 else 768 if p["unit_rows"] == 16 else 512
+        lanes, tiles = 4 if p["tile"] == 32 else 1, -(-tokens // p["tile"])
+        most = min(tokens // (4 * p["tile"]), 4 * places // p["units"] + 1)
+        time = lambda n: -(-p["units"] * n // places) * (-(-tiles // (lanes * n)) + (3 if n > 1 else 0))
+        assert p["n_split"] == min(range(1, max(most, 1) + 1), key=lambda n: (time(n), n))
+
+
 def test_one_token_fills_the_device(rows):
     """One token of one sequence: over a long context on three quarters of the places and more, over
     a short one without partials."""
