@@ -418,12 +418,14 @@ def test_key_bounds(gpu, case, dtype):
 SELECT = [
     (128, 2, 4, 64, 40, 2560, [2560, 2500, 65], 16, 1, 2),
     (128, 1, 1, 32, 9, 280, [288, 33, 0], 4, 0, 1),
-    (64, 3, 8, 32, 300, 9600, [9600, 9000, 8193], 100, 4, 8),          # more blocks than threads
+    (64, 3, 8, 32, 300, 9600, [9600, 9000, 8193], 100, 4, 8),
     (64, 1, 3, 256, 5, 1280, [1280, 1025, -4], 5, 2, 3),
     (128, 1, 64, 32, 40, 1280, [1279], 39, 0, 1),
     (64, 1, 5, 128, 20, 2560, [2433, 1], 1, 0, 1),
     (64, 2, 16, 32, 1100, 35200, [35200, 31], 1024, 0, 1),
     (64, 1, 4, 32, 3001, 96032, [96032, 3300, 40000], 70, 3, 7),       # few of many
+    (64, 1, 3, 32, 5003, 160096, [160096, 130000, 200], 90, 2, 3),
+    (64, 1, 1, 32, 6000, 192000, [192000, 33000], 1100, 0, 1),
     (64, 1, 2, 32, 17003, 544096, [544096, 530000, 7000, 50000], 201, 0, 1),
     (64, 1, 1, 32, 16600, 531200, [531200], 1300, 5, 9),
 ]
