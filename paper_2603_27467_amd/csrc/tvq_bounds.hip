@@ -154,7 +154,7 @@ __global__ __launch_bounds__(kBlockThreads) void key_bounds_kernel(KeyBoundsArgs
 
 // Blocks of a workgroup of block_score_kernel.
 template <int D>
-constexpr uint32_t kScoreBlocks = kBlockThreads / (D / 8) * 4;
+constexpr uint32_t kScoreBlocks = kBlockThreads / (D / 8) * 2;
 
 // Blocks of sequence b's context.
 __device__ __forceinline__ uint32_t context_blocks(const SelectArgs& a, uint32_t b, uint32_t& ctx) {
@@ -185,12 +185,14 @@ __device__ __forceinline__ double lane_xor_f64(double v) {
 }
 
 // Scores of the blocks of one (sequence, KV head): d / 8 lanes per block, 8 channels a lane, so that
-// a wave reads whole rows of bounds, four rounds of 4 (d = 128) or 8 blocks, all requested at the
+// a wave reads whole rows of bounds, two rounds of 4 (d = 128) or 8 blocks, all requested at the
 // start.  Four query heads at a time: their sums over the lanes meet by exchanges that halve the
-// heads a lane looks after twice, then add.
+// heads a lane looks after twice, then add.  Bound by the bounds' bytes: 260,000 blocks of d = 128,
+// 133 MB, 33 us (4 TB/s, what a plain sum of as many bytes reaches; four rounds 36 us); a few blocks
+// by the start, 3.6 us.
 template <int D, bool F32>
 __global__ __launch_bounds__(kBlockThreads) void block_score_kernel(SelectArgs a) {
-  constexpr uint32_t LPB = D / 8, BPW = kWave / LPB, ROUNDS = 4;
+  constexpr uint32_t LPB = D / 8, BPW = kWave / LPB, ROUNDS = 2;
   constexpr uint32_t PER = BPW * ROUNDS * kWavesPerBlock;              // blocks of a workgroup
   static_assert(PER == kScoreBlocks<D>, "the host's grid");
   const uint32_t per_row = (a.n_keys + PER - 1) / PER;
@@ -274,7 +276,8 @@ __global__ __launch_bounds__(kBlockThreads) void block_score_kernel(SelectArgs a
 // so far (most steps end early: as soon as all of a bin are kept).  Counting is what takes the time,
 // as keys next to each other in value fall on one counter.  So with more than 4 keys a thread and no
 // more blocks to keep than threads, the same is done first for the largest key of each thread: at
-// least `want` keys are not below the want-th of those, and only they are counted.
+// least `want` keys are not below the want-th of those, and only they are counted (16,375 keys 15.9
+// us, so 12.7; 3,125 keys, 4 a thread, 6, so 7).
 // A wave looks after KPT x 64 consecutive keys (KPT = 0: of any number, read again in every step),
 // 64 at a time in ascending order, so that places among the kept come from counted ballots.
 template <int THREADS, int KPT>
