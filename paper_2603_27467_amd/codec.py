@@ -306,11 +306,19 @@ class Codec:
         return C.tvq_tensor_desc(t.shape[0], t.shape[2], 0, s[0], s[1], s[2])
 
     @staticmethod
-    def _workspace(workspace, need, device):
-        """The given workspace (the call itself checks its size) or a new one of need() bytes."""
+    def _workspace(workspace, need, device, stream):
+        """The given workspace (the call itself checks its size) or a new one of need() bytes,
+        allocated for the stream that the call runs on."""
         import torch
         if workspace is None:
-            return torch.empty(need(), dtype=torch.uint8, device=device)
+            if stream is None:
+                return torch.empty(need(), dtype=torch.uint8, device=device)
+            if not isinstance(stream, torch.cuda.Stream):
+                handle = _stream_handle(stream)
+                stream = torch.cuda.ExternalStream(handle, device=device) if handle else \
+                    torch.cuda.default_stream(device)
+            with torch.cuda.stream(stream):
+                return torch.empty(need(), dtype=torch.uint8, device=device)
         if workspace.dtype != torch.uint8 or not workspace.is_cuda or \
                 not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous uint8 GPU tensor")
@@ -327,7 +335,8 @@ class Codec:
         dq, do = self._io_dtypes(q, out)
         B, Hq, T, _ = q.shape
         workspace = self._workspace(
-            workspace, lambda: self.attention_prefill_workspace_bytes(B, Hq, T, t_end), q.device)
+            workspace, lambda: self.attention_prefill_workspace_bytes(B, Hq, T, t_end), q.device,
+            stream)
         C.tvq_attention_prefill(self.handle, cache.data_ptr(), lay, layer, t_end, Hq, scale, dq,
                                 q.data_ptr(), self._rows_desc(q), do, out.data_ptr(),
                                 self._rows_desc(out), workspace.data_ptr(), workspace.numel(),
@@ -347,7 +356,8 @@ class Codec:
                 (q_lens is not None and q_lens.shape != (B,)):
             raise ValueError("block_table [B, max_blocks], ctx_lens [B] and q_lens [B] must match q")
         workspace = self._workspace(
-            workspace, lambda: self.attention_prefill_workspace_bytes(B, Hq, T, max_ctx), q.device)
+            workspace, lambda: self.attention_prefill_workspace_bytes(B, Hq, T, max_ctx), q.device,
+            stream)
         C.tvq_attention_prefill_paged(self.handle, pool.data_ptr(), pool_lay,
                                       self._i32(block_table, "block_table"), block_table.shape[1],
                                       self._i32(ctx_lens, "ctx_lens"), max_ctx,
@@ -412,7 +422,8 @@ class Codec:
             raise ValueError("blocks [B, H, n_sel] and sel_lens [B, H] must match q and the codec")
         workspace = self._workspace(
             workspace, lambda: self.select_blocks_workspace_bytes(B, max_ctx,
-                                                                  pool_lay.capacity_tokens), q.device)
+                                                                  pool_lay.capacity_tokens),
+            q.device, stream)
         C.tvq_select_blocks(self.handle, bounds.data_ptr(), pool_lay,
                             self._i32(block_table, "block_table"), table[1],
                             self._i32(ctx_lens, "ctx_lens"), max_ctx, B, layer, Hq, dt,
@@ -442,7 +453,7 @@ class Codec:
         workspace = self._workspace(
             workspace, lambda: self.attention_blocks_workspace_bytes(B, Hq, n_sel,
                                                                      pool_lay.capacity_tokens),
-            q.device)
+            q.device, stream)
         C.tvq_attention_blocks(self.handle, pool.data_ptr(), pool_lay,
                                self._i32(block_table, "block_table"), table[1],
                                self._i32(blocks, "blocks"), n_sel, self._i32(sel_lens, "sel_lens"),

@@ -597,6 +597,41 @@ def test_sparse_step_graph_replay(gpu):
             assert (np.linalg.norm(_f64(graph["o"])[L - 1, b, rows] - ref, axis=1) <= bar).all()
 
 
+@pytest.mark.parametrize("as_handle", [False, True], ids=["stream", "handle"])
+def test_a_workspace_of_the_call_belongs_to_its_stream(gpu, as_handle):
+    """Calls on another stream without a workspace: what the current stream allocates and writes
+    after the call, while it still waits behind other work there, is no part of its workspace."""
+    import torch
+    d, H, B, T, mb = 128, 1, 1, 3, 512
+    p = Pool(["base"], H, d, B, mb, 32, seed=21)
+    ctx = torch.tensor([mb * 32], dtype=torch.int32, device="cuda")
+    q = _randn((B, 4, T, d), 3, torch.bfloat16)
+    want, got = torch.empty_like(q), torch.empty_like(q)
+    ql = q[:, :, 0].contiguous()
+    blocks = torch.arange(mb, dtype=torch.int32, device="cuda").view(1, 1, mb).contiguous()
+    lens = torch.tensor([[mb * 32]], dtype=torch.int32, device="cuda")
+    want_l, got_l = torch.empty_like(ql), torch.empty_like(ql)
+    g = p.s.gpu
+    need = (g.attention_prefill_workspace_bytes(B, 4, T, mb * 32),
+            g.attention_blocks_workspace_bytes(B, 4, mb, 32))
+    assert min(need) > 0
+    g.attention_prefill_paged(p.pool, p.lay, p.table_dev, ctx, mb * 32, 0, q, want, 0.1)
+    g.attention_blocks(p.pool, p.lay, p.table_dev, blocks, lens, 0, ql, want_l, 0.1)
+    side = torch.cuda.Stream()
+    where = side.cuda_stream if as_handle else side
+    busy = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            busy = busy @ busy.T * 1e-4
+    g.attention_prefill_paged(p.pool, p.lay, p.table_dev, ctx, mb * 32, 0, q, got, 0.1, stream=where)
+    g.attention_blocks(p.pool, p.lay, p.table_dev, blocks, lens, 0, ql, got_l, 0.1, stream=where)
+    junk = [torch.full((n,), 0x7F, dtype=torch.uint8, device="cuda") for n in need for _ in range(3)]
+    assert not side.query(), "the calls are still to come"
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(got_l, want_l) and len(junk) == 6
+
+
 def test_bounds_hold_for_the_keys(gpu):
     """What the bounds are for: no key's product with a query is above its block's score."""
     import torch
