@@ -292,15 +292,20 @@ tvq_status tvq_attention_paged(const tvq_codec* c, const void* pool, const tvq_l
  *              <= 0 gives zeros.  The positions below them must lie in blocks the table holds
  *   q_lens     paged: device int32 [B], new tokens per sequence, clipped to 0 .. T; rows behind them
  *              are not written.  NULL: T for all
- *   workspace  device scratch of at least tvq_attention_prefill_workspace(...) bytes, 16-byte
- *              aligned; NULL where that is 0
+ *   workspace  device scratch of at least tvq_attention_prefill_workspace(...) bytes for these
+ *              sizes (more tokens can need less), 16-byte aligned; NULL where that is 0.  It holds
+ *              the partials of spans and, for many rows (at least 4 x 256 per KV head), the rebuilt
+ *              pairs of the whole context, 4 d bytes per token and KV head, while these take at most
+ *              2^31 bytes.  A workspace serves one call at a time
  * The products run on the fp16 matrix cores with fp32 accumulation, operands scaled by powers of
- * two into fp16's range.  bf16 o: queries, rebuilt pairs and softmax weights are rounded to fp16
- * (11 bits) once each.  fp32 o: each is a pair of fp16 numbers (22 bits; expect ~1e-6 relative to
- * an fp64 evaluation).
+ * two into fp16's range.  bf16 o: queries and softmax weights are rounded to fp16 (11 bits) once
+ * each, rebuilt pairs three times (table, norm, product).  fp32 o: each is a pair of fp16 numbers
+ * (22 bits; expect ~1e-6 relative to an fp64 evaluation).  Norms of 2^96 and more can overflow.  A
+ * token whose K or V is not finite may also reach rows that do not see it.
  * Supported: d = 64 or 128, at most 64 query heads per KV head, n = 64, 128 or 256 with 8-bit linear
  * or 4-bit log-space norms for both K and V of the layer (TVQ_ERR_UNSUPPORTED otherwise).  Launches
- * one kernel on `stream`, two where the workspace is not empty; T == 0 launches nothing. */
+ * one to three kernels on `stream` (the rebuilding, the attention, the merge of spans), the same ones
+ * for the same sizes; T == 0 launches nothing. */
 tvq_status tvq_attention_prefill_workspace(const tvq_codec* c, int64_t batch, int32_t num_q_heads,
                                            int64_t tokens, int64_t max_ctx, int64_t* bytes);
 tvq_status tvq_attention_prefill(const tvq_codec* c, const void* cache, const tvq_layout* lay,
@@ -339,8 +344,9 @@ tvq_status tvq_key_bounds_paged(const tvq_codec* c, tvq_dtype in_dtype, const vo
  * score highest, score(i) = max over the head's query heads of
  *   sum_c max(q_c, 0) hi_ic + min(q_c, 0) lo_ic,
  * an upper bound of q . k over the keys of block i; the sum in fp64, rounded to fp32.  A query head
- * with an element that is not finite scores lowest, ties go to the lower block.  The first n_first blocks and the last n_last are
- * always among them (n_first >= 0, n_last >= 1, n_first + n_last <= n_sel).
+ * with an element that is not finite scores lowest, ties go to the lower block.  The first n_first
+ * blocks and the last n_last are always among them (n_first >= 0, n_last >= 1, n_first + n_last <=
+ * n_sel).
  *   q          device [B][num_q_heads][d], contiguous, bf16 or fp32, 16-byte aligned
  *   ctx_lens   device int32 [B], clipped to max_ctx (1 .. max_blocks * block_tokens)
  *   blocks     device int32 [B][H][n_sel]: block numbers of the sequence (its table's entries) in

@@ -72,7 +72,10 @@ struct RowsPlan {
 };
 
 // Rebuilding the tiles of all tokens once costs a launch and 4 d bytes a token and head written and
-// read back; every unit but one of a (sequence, KV head) is spared it.
+// read back; every unit but one of a (sequence, KV head) is spared it.  Two sequences of 8,000 tokens,
+// 8 KV heads, d = 128, us with tiles of each unit's own and kept: 2 units 70 and 77, 3 units 90 and
+// 94, 4 units 107 and 106, 5 units 128 and 125, 7 units 177 and 164.  fp32 outputs would need twice
+// the bytes and rebuild their own.
 constexpr int64_t kRebuildUnits = 4;                 // units from which on the tiles are kept
 constexpr int64_t kRebuildBytes = 1ll << 31;         // and the most they may take
 
@@ -80,11 +83,19 @@ constexpr int64_t kRebuildBytes = 1ll << 31;         // and the most they may ta
 // context; d: head dimension; cus: compute units.
 //
 // Up to 32 rows the four waves of a workgroup take tokens of their own, in tiles of 32 (units of 16 or
-// 32 rows); above, four or eight waves of 32 rows each share tiles of 64.
-// The spans of a launch go to the places that the device has for its workgroups, so many at a time;
-// a span costs its tiles and, for its start and its partial, about kSpanTiles more.  The number of
-// spans with the least time for full contexts is taken, of at least 4 tiles each (one a wave where
-// the waves take tokens of their own).
+// 32 rows); above, four or eight waves of 32 rows each share tiles of 64.  Measured on both sides, us,
+// 8 KV heads, d = 128:
+//   4 rows, 64 blocks of 16 sequences      units of 16 rows 44, of 32 rows 55
+//   20 rows, 8 sequences of 4,100 tokens   tokens of their own 38, shared tiles 45
+//   32 rows, a sequence of 16,000          tokens of their own 30, shared tiles 35
+//   128 rows, 8 sequences of 4,100         four waves 54, eight 59
+//   256 rows, 8 sequences of 4,100         four waves (two units) 85, eight 70
+// The spans of a launch go to the places that the device has for its workgroups (by their registers
+// and LDS: three a compute unit with units of 16 rows, one with eight waves, else two), so many at a
+// time; a span costs its tiles and, for its start and its partial, about kSpanTiles more.  The number
+// of spans with the least time for full contexts is taken, of at least 4 tiles each (one a wave where
+// the waves take tokens of their own).  1, 3 and 6 for kSpanTiles are alike but for 448 tokens behind
+// 7,552 of two sequences: 199, 164 and 164 us.
 constexpr int64_t kSpanTiles = 3;
 
 inline RowsPlan rows_plan(int64_t batch, int64_t heads, int64_t rows, int64_t tokens, int32_t d,

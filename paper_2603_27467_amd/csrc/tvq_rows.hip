@@ -5,8 +5,14 @@
 // As in tvq_attention.hip the work is done in the rotated domain,
 //   s_t = (scale W D q) . y'_K,t     o = D W (sum_t p_t y'_V,t) / sum_t p_t,
 // with y' the rebuilt pairs, 1/sqrt(d) folded in: one butterfly per query row and one per output
-// row.  With 32 rows and more per KV head the two products are matrix products, and a rebuilt tile
-// of keys and values serves all rows of the workgroup.
+// row.  Both products are matrix products over tiles of rebuilt keys and values in LDS, which serve
+// all rows of a workgroup.  How a call is cut up, and which kernel it takes, stands in tvq_rows.h:
+//   few_rows_kernel    up to 32 query rows per KV head: the waves take tokens of their own
+//   rows_kernel        more: the waves take 32 rows each and share the tiles they rebuild together
+//   rows_many_kernel   many, bf16 outputs: the same on tiles that rows_tiles_kernel rebuilt once
+//   rows_merge_kernel, rows_merge_many_kernel   the partials of spans
+// A rebuilt pair costs 6 to 7 vector instructions however many rows use it: few rows are bound by the
+// rebuilding, many by the products.
 //
 // Arithmetic.  The products run on v_mfma_f32_32x32x16_f16 with fp32 accumulation; scores, softmax
 // statistics and accumulators are fp32.  fp16 keeps 11 bits of an operand, three more than bf16, at
@@ -20,8 +26,8 @@
 // Where o is fp32 each operand is the sum of two fp16 numbers (22 bits) and the products are the
 // three that matter: hi hi + hi lo + lo hi.
 //
-// Layout of the instruction (A 32 x 16, B 16 x 32): lane l gives row (A) or column (B) l % 32 and
-// the 8 k's 8 (l / 32) ..; register i of the result is row (i % 4) + 8 (i / 4) + 4 (l / 32), column
+// Layout of v_mfma_f32_32x32x16_f16 (A 32 x 16, B 16 x 32): lane l gives row (A) or column (B) l % 32
+// and the 8 k's 8 (l / 32) ..; register i of the result is row (i % 4) + 8 (i / 4) + 4 (l / 32), column
 // l % 32.
 //   scores  A = y'_K (rows: 32 tokens, k: elements) from LDS, B = q^ in registers: a lane holds 16
 //           scores of one query row, so maximum and sum are in-lane but for one exchange of the
@@ -34,8 +40,8 @@
 //
 // Tiles.  A wave rebuilds 64 / (d / 32) tokens at once, d / 32 lanes per token, 16 pairs a lane,
 // into LDS rows of d fp16 (hi and lo planes), 16-byte chunks permuted by the token so that reads
-// by token and the transposing reads meet no bank twice.  The codes of the next tile are requested
-// before the current one is worked on.
+// by token and the transposing reads meet no bank twice.  (Copies of the tables against conflicts of
+// the gathers, 2 to 8 of them, change nothing.)
 //
 // m of a row is a reference point: it is raised, and sum and accumulators rescaled, only when a
 // score exceeds it by more than kLazy (log2 units); weights stay below 2^(kLazy + kBias) and
@@ -337,18 +343,17 @@ __device__ __forceinline__ void store_row(const RowsArgs& a, uint64_t at, float 
   }
 }
 
-// q^ = scale W D q of the lane's row as fp16 parts; LPR lanes of the wave hold a row (its place among
-// them is `part`), elements 8 LPR k + 8 part + i at [k][i].  Returns the power of two that the scores
-// must be multiplied by.
-template <int D, int PARTS, int LPR>
-__device__ __forceinline__ float load_rows(const RowsArgs& a, uint64_t at, int lane,
-                                           h8 (&q)[PARTS][D / (8 * LPR)]) {
-  constexpr int N = D / LPR;
-  const int part = lane / (kWave / LPR);
+// q^ = scale W D q of the lane's row as fp16 parts; the lanes l and l + 32 hold a row, elements 16 k +
+// 8 half + i at [k][i].  Returns the power of two that the scores must be multiplied by.
+template <int D, int PARTS>
+__device__ __forceinline__ float load_row(const RowsArgs& a, uint64_t at, int lane,
+                                          h8 (&q)[PARTS][D / 16]) {
+  constexpr int N = D / 2;
+  const int half = lane >> 5;
   float x[N];
 #pragma unroll
   for (int k = 0; k < N / 8; ++k) {
-    const int e = 8 * LPR * k + 8 * part;
+    const int e = 16 * k + 8 * half;
     const u32x4a s = *(const u32x4a*)(a.signs + e / 2);
     if (a.q_f32) {
       const float* p = (const float*)a.q + at + e;
@@ -369,18 +374,13 @@ __device__ __forceinline__ float load_rows(const RowsArgs& a, uint64_t at, int l
   }
 #pragma unroll
   for (int h = 1; h < N; h <<= 1) stage_regs(x, h);
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    if constexpr (LPR == 4) x[j] = fwht_stage<16>(x[j], lane);
-    x[j] = fwht_stage<32>(x[j], lane);
-  }
   float top = 0.0f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    x[i] *= a.qscale;
+    x[i] = fwht_stage<32>(x[i], lane) * a.qscale;
     top = fmaxf(top, fabsf(x[i]));
   }
-  top = over_row<LPR>(top, [](float u, float v) { return fmaxf(u, v); });
+  top = over_row<2>(top, [](float u, float v) { return fmaxf(u, v); });
   // largest element in [2^7, 2^8)
   const int e = min(max((int)(__float_as_uint(top) >> 23) - 127 - 7, -119), 120);
   const float down = pow2i(-e);
@@ -430,7 +430,7 @@ struct Rows {
     lim_hi = (uint32_t)__builtin_amdgcn_readlane((int)lim, 31);
     const uint64_t at = (uint64_t)u.b * a.q_stride[0] + (uint64_t)(u.h * a.G + g) * a.q_stride[1] +
                         (uint64_t)j * a.q_stride[2];
-    qf = load_rows<D, PARTS, 2>(a, at, lane, q);
+    qf = load_row<D, PARTS>(a, at, lane, q);
     m = kNoScore;
     l = 0.0f;
     vexp = kNoExp;
@@ -683,6 +683,9 @@ struct RowsWave {
 // Every workgroup rebuilds its own tiles; 32 rows a wave.  Eight waves have two tiles in LDS and
 // rebuild the next before they use the current one, one wait a tile; fewer waves, several of whose
 // workgroups share a compute unit, rebuild a tile and then use it.
+// 8 sequences, 4,100 tokens, 8 KV heads, d = 128: 64 rows each 50 us, 128 rows 55 (196 TFLOP/s), 256
+// rows 70 (304); two prompts of 2,047 tokens, 4 KV heads, d = 64, fp32 107 us, 17 GFLOP of scores and
+// sums at three products each (480 TFLOP/s), the last units' 32 tiles one after another.
 template <int D, int WAVES, int PARTS>
 __global__ __launch_bounds__(WAVES * kWave, 2) void rows_kernel(RowsArgs a) {
   using S = Shape<D, WAVES, PARTS>;
@@ -767,7 +770,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void rows_kernel(RowsArgs a) {
 }
 
 // The tiles of a call's tokens, rebuilt once into the workspace as rows_many_kernel holds them in LDS,
-// with their E's: a tile per workgroup, by way of LDS so that whole cache lines are stored.
+// with their E's: a tile per workgroup, by way of LDS so that whole cache lines are stored.  Bound by
+// the stores: 32,700 tokens, 8 heads, d = 128, 134 MB in 42 us (3.2 TB/s).
 template <int D>
 __global__ __launch_bounds__(kBlockThreads) void rows_tiles_kernel(RowsArgs a) {
   using S = Shape<D, 4, 1>;
@@ -800,6 +804,9 @@ __global__ __launch_bounds__(kBlockThreads) void rows_tiles_kernel(RowsArgs a) {
 // its products: the keys of i + 2 before the value products of i, the values of i + 1 after them.
 // In the middle of tile t the waves meet: tile t + 1 is then complete and tile t - 1 read, and its
 // place is taken by t + 2, which was requested a tile before.
+// 1,025 tokens behind 31,675, 8 KV heads of 4, d = 128: 540 GFLOP in 690 to 740 us (730 to 780
+// TFLOP/s; the library's product of 8192 reaches 1,187).  The clock falls to 2.04 GHz under it: power
+// bounds it, and neither earlier reads, 64 rows a wave nor other orders of the phases gain.
 template <int D>
 __global__ __launch_bounds__(8 * kWave, 2) void rows_many_kernel(RowsArgs a) {
   using S = Shape<D, 8, 1>;
@@ -1046,8 +1053,14 @@ struct QueryPiece {
 // Up to 16 NR query rows per KV head: four waves, each on tokens of its own in a tile of 32 of its own,
 // which holds the keys and then, once the scores are there, the values.  No waits between the waves;
 // their sums meet in LDS at the end, and a row is finished by one wave.
+// 16 sequences, 64 blocks of 64 tokens for each of 8 KV heads of 4, d = 128: 112 MB of codes in 38 us
+// (2.9 TB/s); five draft tokens (20 rows, NR = 2) behind 4,100 tokens of 8 sequences 31 us.  Of a
+// wave's time 40 % are vector instructions, nearly all of them the rebuilding, and 40 % waits for LDS
+// and memory with two or three waves on a SIMD; requesting the codes a whole tile ahead, q^ in LDS
+// for a third wave and four waves a SIMD were each slower (their registers do not fit).
 template <int D, int PARTS, int NR>
-__global__ __launch_bounds__(kBlockThreads, PARTS * NR == 1 ? 3 : PARTS * NR == 4 ? 1 : 2) void few_rows_kernel(RowsArgs a) {
+__global__ __launch_bounds__(kBlockThreads, PARTS * NR == 1 ? 3 : PARTS * NR == 4 ? 1 : 2)
+void few_rows_kernel(RowsArgs a) {
   using S = Shape<D, 4, PARTS>;
   typedef float v4f __attribute__((ext_vector_type(4)));
   constexpr int TILE = 32, NG = TILE / S::GROUP, PLANE = TILE * S::ROW, PITCH = D + 4;
@@ -1243,7 +1256,8 @@ __global__ __launch_bounds__(kBlockThreads, PARTS * NR == 1 ? 3 : PARTS * NR == 
 
 // The spans of one row, a row per wave, its elements across the lanes: M = max m, then
 // o = D W (sum 2^(m - M) acc) / (sum 2^(m - M) l).  The spans' (m, l) are read 64 at a time, one
-// per lane, and 8 spans' rows are requested together, the first ones before M is known.
+// per lane, and 8 spans' rows are requested together, the first ones before M is known.  Bound by the
+// launch: 4 us.
 template <int D>
 __global__ __launch_bounds__(kBlockThreads) void rows_merge_kernel(RowsArgs a) {
   constexpr int EPL = D / kWave;
@@ -1302,8 +1316,9 @@ __global__ __launch_bounds__(kBlockThreads) void rows_merge_kernel(RowsArgs a) {
 
 // The same for units of 256 rows: kMergeRows rows a wave, four at a time, a row on 16 lanes, d / 16
 // elements each, and 8 of its spans requested together.  A launch has so many rows then that what
-// each wave finds out first is most of a row per wave: 32 000 rows of 4 spans took 18.8 us, so 11.6.  Units
-// of fewer rows are merged faster by a wave per row (8 heads of 80 rows of 63 spans: 8 us, so 16).
+// each wave finds out first is most of a row per wave: 32,000 rows of 4 spans took 18.8 us, so 11.6.
+// Units of fewer rows are merged faster by a wave per row (8 heads of 80 rows of 63 spans: 8 us, so
+// 16).
 constexpr uint32_t kMergeRows = 8;
 
 template <int D>
