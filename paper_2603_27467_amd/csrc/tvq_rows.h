@@ -94,9 +94,11 @@ constexpr int64_t kRebuildBytes = 1ll << 31;         // and the most they may ta
 // and LDS: three a compute unit with units of 16 rows, one with eight waves, else two), so many at a
 // time; a span costs its tiles and, for its start and its partial, about kSpanTiles more.  The number
 // of spans with the least time for full contexts is taken, of at least 4 tiles each (one a wave where
-// the waves take tokens of their own).  1, 3 and 6 for kSpanTiles are alike but for 448 tokens behind
-// 7,552 of two sequences: 199, 164 and 164 us.
-constexpr int64_t kSpanTiles = 3;
+// the waves take tokens of their own).  us for several values of kSpanTiles: 448 tokens behind 7,552
+// of two sequences 199 (1), 164 (3), 164 (6); with tokens of their own, one token over 512 of a
+// sequence 13.2 (1), 13.2 (2), 16.7 (3) and over 256 13.2 (0), 10.9 (2), over 512 of 32 sequences 19.7
+// (1), 18.7 (2), 18.7 (3).
+constexpr int64_t kSpanTiles[2] = {3, 2};            // shared tiles; tokens of their own
 
 inline RowsPlan rows_plan(int64_t batch, int64_t heads, int64_t rows, int64_t tokens, int32_t d,
                           int64_t cus) {
@@ -118,7 +120,7 @@ inline RowsPlan rows_plan(int64_t batch, int64_t heads, int64_t rows, int64_t to
   int64_t best = 1, least = ceil_div(p.units, places) * ceil_div(tiles, lanes);
   for (int64_t n = 2; n <= most && n <= fill;) {
     const int64_t per = ceil_div(tiles, lanes * n);
-    const int64_t time = ceil_div(p.units * n, places) * (per + kSpanTiles);
+    const int64_t time = ceil_div(p.units * n, places) * (per + kSpanTiles[few]);
     if (time < least) best = n, least = time;
     if (per == 1) break;
     n = ceil_div(tiles, lanes * (per - 1));           // more spans of as many tiles save nothing

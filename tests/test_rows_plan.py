@@ -91,7 +91,7 @@ def test_plans(rows):
 
 def test_the_number_of_spans_takes_the_least_time(rows):
     """Against the rule over every number: rounds of the device's places, times the tiles of a span
-    and three more where there are several."""
+    and three more (two where the waves take tokens of their own) where there are several."""
     rng = np.random.default_rng(3)
     for _ in range(400):
         lines, n_rows = int(math.exp(rng.uniform(0, 5))), int(math.exp(rng.uniform(0, 8)))
@@ -100,7 +100,8 @@ def test_the_number_of_spans_takes_the_least_time(rows):
         places = 256 if p["waves"] == 8 else 768 if p["unit_rows"] == 16 else 512
         lanes, tiles = 4 if p["tile"] == 32 else 1, -(-tokens // p["tile"])
         most = min(tokens // (4 * p["tile"]), 4 * places // p["units"] + 1)
-        time = lambda n: -(-p["units"] * n // places) * (-(-tiles // (lanes * n)) + (3 if n > 1 else 0))
+        cut = 2 if lanes == 4 else 3
+        time = lambda n: -(-p["units"] * n // places) * (-(-tiles // (lanes * n)) + (cut if n > 1 else 0))
         assert p["n_split"] == min(range(1, max(most, 1) + 1), key=lambda n: (time(n), n))
 
 
