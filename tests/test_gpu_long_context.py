@@ -632,6 +632,53 @@ def test_a_workspace_of_the_call_belongs_to_its_stream(gpu, as_handle):
     assert torch.equal(got, want) and torch.equal(got_l, want_l) and len(junk) == 6
 
 
+def test_graphs_that_share_a_workspace(gpu):
+    """A prompt chunk (tiles kept in the workspace, spans, merge) and a token over listed blocks,
+    captured each into a graph of its own with one workspace and replayed in turn on new queries and
+    lengths, against eager calls with workspaces of their own."""
+    import torch
+    d, H, G, B, P, mb, T = 64, 1, 16, 2, 32, 40, 70
+    p = Pool(["n64"], H, d, B, mb, P, seed=31)
+    g, max_ctx = p.s.gpu, mb * P
+    ctx = torch.tensor([max_ctx, 700], dtype=torch.int32, device="cuda")
+    new = torch.tensor([T, 33], dtype=torch.int32, device="cuda")
+    q, ql = _randn((B, H * G, T, d), 1, torch.bfloat16), _randn((B, H * G, d), 2, torch.float32)
+    o, ol = torch.zeros_like(q), torch.zeros_like(ql)
+    blocks = torch.arange(mb, dtype=torch.int32, device="cuda").flip(0).expand(B, H, mb).contiguous()
+    lens = torch.tensor([[max_ctx - 5], [900]], dtype=torch.int32, device="cuda")
+    need = (g.attention_prefill_workspace_bytes(B, H * G, T, max_ctx),
+            g.attention_blocks_workspace_bytes(B, H * G, mb, P))
+    assert min(need) > 0
+    ws = torch.empty(max(need), dtype=torch.uint8, device="cuda")
+    chunk = lambda out, w: g.attention_prefill_paged(p.pool, p.lay, p.table_dev, ctx, max_ctx, 0, q, out,
+                                                     0.1, q_lens=new, workspace=w)
+    token = lambda out, w: g.attention_blocks(p.pool, p.lay, p.table_dev, blocks, lens, 0, ql, out, 0.1,
+                                              workspace=w)
+    side, graphs = torch.cuda.Stream(), []
+    side.wait_stream(torch.cuda.current_stream())
+    for call, out in ((chunk, o), (token, ol)):
+        with torch.cuda.stream(side):
+            call(out, ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(out, ws)
+        graphs.append(graph)
+    for step in range(4):
+        q.copy_(_randn(q.shape, 10 + step, q.dtype))
+        ql.copy_(_randn(ql.shape, 20 + step, ql.dtype))
+        ctx.copy_(torch.tensor([max_ctx - 100 * step, 70 + step], dtype=torch.int32))
+        lens.add_(-100)
+        o.zero_(), ol.zero_()
+        for graph in graphs if step % 2 else graphs[::-1]:
+            graph.replay()
+        want, want_l = torch.zeros_like(o), torch.zeros_like(ol)
+        chunk(want, None), token(want_l, None)
+        torch.cuda.synchronize()
+        assert torch.equal(o, want) and torch.equal(ol, want_l), step
+        assert (o != 0).any() and (ol != 0).any()
+
+
 def test_bounds_hold_for_the_keys(gpu):
     """What the bounds are for: no key's product with a query is above its block's score."""
     import torch
