@@ -271,15 +271,12 @@ __global__ __launch_bounds__(kBlockThreads) void block_score_kernel(SelectArgs a
 }
 
 // The n_sel largest keys of one (sequence, KV head), the lower block first among equals; the first
-// and last blocks stand outside the comparison.  With x = key - smallest key, the x of the last
-// kept block is found from its top down, 8 bits a step, by counting the x that share the bits found
-// so far (most steps end early: as soon as all of a bin are kept).  Counting is what takes the time,
-// as keys next to each other in value fall on one counter.  So with more than 4 keys a thread and no
-// more blocks to keep than threads, the same is done first for the largest key of each thread: at
-// least `want` keys are not below the want-th of those, and only they are counted (16,375 keys 15.9
-// us, so 12.7; 3,125 keys, 4 a thread, 6, so 7).
-// A wave looks after KPT x 64 consecutive keys (KPT = 0: of any number, read again in every step),
-// 64 at a time in ascending order, so that places among the kept come from counted ballots.
+// and last blocks stand outside the comparison.  The key of the last kept block is found from its
+// top down, 8 bits a step, by counting the keys of the range that is left by their next 8 bits (most
+// steps end early: as soon as all of a bin are kept).  A wave looks after KPT x 64 consecutive keys
+// (KPT = 0: of any number, read again in every step), 64 at a time in ascending order, so that places
+// among the kept come from counted ballots.  Bound by the vector instructions of its one workgroup,
+// six passes over the keys.
 template <int THREADS, int KPT>
 __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
   constexpr uint32_t WAVES = THREADS / kWave;
@@ -318,73 +315,62 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
 #pragma unroll
       for (int c = 0; c < KPT; ++c) f(first + c * kWave, k[c], first + c * kWave < m);
     } else {
-      for (uint32_t c = 0, i = first; c < per; ++c, i += kWave) f(i, keys[min(i, m - 1)], i < m);
-    }
-  };
-  uint32_t left;                                   // bits of x = key - low yet to find
-  uint32_t need = want;                            // kept among those that share the bits found
-  // The bits found of the need-th largest x among those that `visit` hands out, in `steps` steps.
-  auto find = [&](auto&& visit, uint32_t low, uint32_t steps) {
-    uint32_t found = 0;
-    for (; left > 0 && steps > 0; --steps) {
-      const uint32_t w = min(left, 8u), sh = left - w;
-      __syncthreads();                             // s_wave and s_pick are read
-      for (uint32_t i = t; i < 256; i += THREADS) s_hist[i] = 0;
-      __syncthreads();
-      visit([&](uint32_t, uint32_t x, bool there) {
-        const uint64_t v = x - low;
-        if (there && x >= low && (v >> left) == found)
-          atomicAdd(&s_hist[(uint32_t)(v >> sh) & ((1u << w) - 1u)], 1u);
-      });
-      __syncthreads();
-      if (wave == 0) {                             // lane l: bins 255 - 4 l down to 252 - 4 l
-        const uint4 v = *(const uint4*)(s_hist + 252 - 4 * lane);
-        const uint32_t sum = v.x + v.y + v.z + v.w;
-        const uint32_t end = wave_scan(sum);
-        uint32_t before = end - sum;
-        if (before < need && end >= need) {
-          const uint32_t c[4] = {v.w, v.z, v.y, v.x};
-          uint32_t i = 0;
-          while (before + c[i] < need) before += c[i++];
-          s_pick[0] = 255 - 4 * lane - i, s_pick[1] = before, s_pick[2] = c[i];
-        }
+      constexpr uint32_t AT_ONCE = 8;
+      for (uint32_t c = 0, i = first; c < per; c += AT_ONCE, i += AT_ONCE * kWave) {
+        uint32_t x[AT_ONCE];
+#pragma unroll
+        for (uint32_t j = 0; j < AT_ONCE; ++j) x[j] = keys[min(i + j * kWave, m - 1)];
+#pragma unroll
+        for (uint32_t j = 0; j < AT_ONCE; ++j) f(i + j * kWave, x[j], c + j < per && i + j * kWave < m);
       }
-      __syncthreads();
-      found = (found << w) | s_pick[0];
-      need -= s_pick[1];
-      left = sh;
-      if (s_pick[2] == need) break;                // all of the bin are kept
     }
-    return found;
   };
-  const uint32_t share = per * kWave;
-  const uint32_t threads = m / share * kWave + min(m % share, (uint32_t)kWave);    // with keys
-  const bool prune = KPT != 4 && want <= threads;
-  uint32_t least = 0xFFFFFFFFu, most = 0;
+  uint32_t base = 0xFFFFFFFFu, top = 0;
   each([&](uint32_t, uint32_t x, bool there) {
-    if (there) least = min(least, x), most = max(most, x);
+    if (there) base = min(base, x), top = max(top, x);
   });
-  uint32_t low = prune && first < m ? most : least, top = most;
 #pragma unroll
   for (int s = 1; s < kWave; s <<= 1) {
-    low = min(low, (uint32_t)__shfl_xor((int)low, s));
+    base = min(base, (uint32_t)__shfl_xor((int)base, s));
     top = max(top, (uint32_t)__shfl_xor((int)top, s));
   }
-  if (lane == 0) s_wave[0][wave] = low, s_wave[1][wave] = top;
+  if (lane == 0) s_wave[0][wave] = base, s_wave[1][wave] = top;
   __syncthreads();
-  for (uint32_t w = 0; w < WAVES; ++w) low = min(low, s_wave[0][w]), top = max(top, s_wave[1][w]);
-  auto bits = [&]() { return top == low ? 0u : 32u - (uint32_t)__builtin_clz(top - low); };
-  left = bits();
-  if (prune) {
-    const uint32_t found = find([&](auto&& f) { f(first, most, first < m); }, low, 2);
-    low += found << left;
-    left = bits();
-    need = want;
+  for (uint32_t w = 0; w < WAVES; ++w) base = min(base, s_wave[0][w]), top = max(top, s_wave[1][w]);
+  // the range [base, base + span] that holds the key, inside [.., top], so that one comparison tells
+  uint32_t span = top - base, need = want;         // need: kept among the keys of the range
+  uint32_t left = span == 0 ? 0u : 32u - (uint32_t)__builtin_clz(span);             // bits to find
+  while (left > 0) {
+    const uint32_t sh = left - min(left, 8u);
+    __syncthreads();                               // s_wave and s_pick are read
+    for (uint32_t i = t; i < 256; i += THREADS) s_hist[i] = 0;
+    __syncthreads();
+    each([&](uint32_t, uint32_t x, bool there) {
+      if (there && x - base <= span) atomicAdd(&s_hist[(x - base) >> sh], 1u);
+    });
+    __syncthreads();
+    if (wave == 0) {                               // lane l: bins 255 - 4 l down to 252 - 4 l
+      const uint4 v = *(const uint4*)(s_hist + 252 - 4 * lane);
+      const uint32_t sum = v.x + v.y + v.z + v.w;
+      const uint32_t end = wave_scan(sum);
+      uint32_t before = end - sum;
+      if (before < need && end >= need) {
+        const uint32_t c[4] = {v.w, v.z, v.y, v.x};
+        uint32_t i = 0;
+        while (before + c[i] < need) before += c[i++];
+        s_pick[0] = 255 - 4 * lane - i, s_pick[1] = before, s_pick[2] = c[i];
+      }
+    }
+    __syncthreads();
+    base += s_pick[0] << sh;
+    span = min((1u << sh) - 1u, top - base);
+    need -= s_pick[1];
+    left = sh;
+    if (s_pick[2] == need) break;                  // all of the bin are kept
   }
-  const uint32_t found = find(each, low, 4);
-  // kept: x >> left above `found`, and the first `need` that equal it
-  auto above = [&](uint32_t x, bool there) { return there && x >= low && (x - low) >> left > found; };
-  auto equal = [&](uint32_t x, bool there) { return there && x >= low && (x - low) >> left == found; };
+  // kept: the keys above the range, and the first `need` in it
+  auto above = [&](uint32_t x, bool there) { return there && x > base + span; };
+  auto equal = [&](uint32_t x, bool there) { return there && x - base <= span; };
   uint32_t na = 0, ne = 0;
   each([&](uint32_t, uint32_t x, bool there) {
     na += __popcll(__builtin_amdgcn_ballot_w64(above(x, there)));
@@ -431,8 +417,8 @@ void launch_scores(const SelectArgs& a, hipStream_t s) {
 }
 
 // The keys of a list stay in registers where 1024 threads can hold them, of the fewest that do: a list
-// of 129 keys takes 4.1 us on 256 threads of 4 and 11 on 1024 of 16; 3,125 keys 6 on 1024 of 4, 9 read
-// again in every step, 11.5 on 1024 of 16; 16,375 keys 12.7 on 1024 of 16 and 23 read again.
+// of 129 keys takes 3.8 us on 256 threads of 4, 4.9 on 1024 of 4 and 7.7 on 1024 of 16; 3,125 keys 5.4
+// on 1024 of 4, 8.7 on 1024 of 16; 16,375 keys 9.5 on 1024 of 16 and 13.2 read again in every step.
 void launch_select(const SelectArgs& a, hipStream_t s) {
   const dim3 grid(a.B * a.H);
   if (a.n_keys <= 256 * 4)

@@ -113,7 +113,7 @@ PREFILL = [
     (128, 2, 16, "log", 32, 7, 224, [224], 66, None),
     (64, 2, 8, "swapped", 128, 6, 700, [768, 129], 130, [130, 129]),
     (64, 1, 32, "early8", 32, 3, 96, [95, 1, 33], 33, [33, 1, 0]),
-    # units that shares cut, more than 64 of them, a unit per workgroup, units that see nothing
+    # units of several spans, more than 64 units, units that see nothing
     (128, 1, 64, "base", 64, 32, 2048, [2048, 100], 260, [260, 100]),
     (64, 2, 64, "n64", 32, 10, 300, [300, 40, 0], 256, [256, 100, 5]),
     (128, 1, 8, "log", 64, 40, 2500, [2500, 70, 1000], 300, [300, 300, 200]),
