@@ -354,7 +354,7 @@ tvq_status tvq_key_bounds_paged(const tvq_codec* c, tvq_dtype in_dtype, const vo
  *   sel_lens   device int32 [B][H]: the tokens of the context in these blocks
  *   workspace  tvq_select_blocks_workspace(...) bytes, 16-byte aligned
  * A table entry that holds no pool block is read as block 0.  n_sel <= 65536, and at most 64 query
- * heads per KV head.  Two kernel launches. */
+ * heads per KV head.  One kernel launch for short lists, else two; the same for the same sizes. */
 tvq_status tvq_select_blocks_workspace(const tvq_codec* c, int64_t batch, int64_t max_ctx,
                                        int64_t block_tokens, int64_t* bytes);
 tvq_status tvq_select_blocks(const tvq_codec* c, const void* bounds, const tvq_layout* pool_layout,

@@ -1270,6 +1270,7 @@ tvq_status tvq_select_blocks(const tvq_codec* c, const void* bounds, const tvq_l
   a.n_first = (uint32_t)n_first;
   a.n_last = (uint32_t)n_last;
   a.keys = (uint32_t*)workspace;
+  a.cus = (uint32_t)std::max(c->n_cu, 1);
   a.blocks = blocks;
   a.lens = sel_lens;
   const int rc = tvq_launch_select(a, c->d, q_dtype == TVQ_F32, stream);

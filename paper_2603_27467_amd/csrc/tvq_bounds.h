@@ -29,6 +29,7 @@ struct SelectArgs {
   uint32_t* keys;                         // [B*H][n_keys]
   int32_t* blocks;                        // [B*H][n_sel]
   int32_t* lens;                          // [B*H]
+  uint32_t cus;            // compute units
 };
 
 }  // namespace tvq

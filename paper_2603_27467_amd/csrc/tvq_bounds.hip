@@ -152,10 +152,6 @@ __global__ __launch_bounds__(kBlockThreads) void key_bounds_kernel(KeyBoundsArgs
   *(u32x4a*)(out + D) = *(const u32x4a*)hi;
 }
 
-// Blocks of a workgroup of block_score_kernel.
-template <int D>
-constexpr uint32_t kScoreBlocks = kBlockThreads / (D / 8) * 2;
-
 // Blocks of sequence b's context.
 __device__ __forceinline__ uint32_t context_blocks(const SelectArgs& a, uint32_t b, uint32_t& ctx) {
   const int32_t len = a.pg.seq[b];
@@ -184,39 +180,31 @@ __device__ __forceinline__ double lane_xor_f64(double v) {
   return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
 }
 
-// Scores of the blocks of one (sequence, KV head): d / 8 lanes per block, 8 channels a lane, so that
-// a wave reads whole rows of bounds, two rounds of 4 (d = 128) or 8 blocks, all requested at the
-// start.  Four query heads at a time: their sums over the lanes meet by exchanges that halve the
-// heads a lane looks after twice, then add.  Bound by the bounds' bytes: 260,000 blocks of d = 128,
-// 133 MB, 33 us (4 TB/s, what a plain sum of as many bytes reaches; four rounds 36 us); a few blocks
-// by the start, 3.6 us.
+constexpr uint32_t kHeadRounds = 2;
+
+// The part of a wave in the scores: d / 8 lanes per block, 8 channels a lane, so that a wave reads
+// whole rows of bounds, 4 (d = 128) or 8 blocks at a time.  Four query heads at a time: their sums
+// over the lanes meet by exchanges that halve the heads a lane looks after twice, then add.
 template <int D, bool F32>
-__global__ __launch_bounds__(kBlockThreads) void block_score_kernel(SelectArgs a) {
-  constexpr uint32_t LPB = D / 8, BPW = kWave / LPB, ROUNDS = 2;
-  constexpr uint32_t PER = BPW * ROUNDS * kWavesPerBlock;              // blocks of a workgroup
-  static_assert(PER == kScoreBlocks<D>, "the host's grid");
-  const uint32_t per_row = (a.n_keys + PER - 1) / PER;
-  const uint32_t row = blockIdx.x / per_row;
-  const uint32_t b = row / a.H, h = row - b * a.H;
-  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const uint32_t sub = lane % LPB;
-  const uint32_t i0 = (blockIdx.x - row * per_row) * PER + wave * BPW * ROUNDS + lane / LPB;
-  uint32_t ctx;
-  const uint32_t n = context_blocks(a, b, ctx);
-  if (i0 - lane / LPB >= n) return;
-  u32x4a lo[ROUNDS], hi[ROUNDS];
-#pragma unroll
-  for (uint32_t r = 0; r < ROUNDS; ++r) {
-    const uint32_t i = min(i0 + r * BPW, n - 1);
+struct Scorer {
+  static constexpr uint32_t LPB = D / 8, BPW = kWave / LPB;            // lanes of a block, blocks of a wave
+  const SelectArgs& a;
+  const uint32_t row, b, h, lane, sub;
+  double q[4][8];
+
+  __device__ __forceinline__ Scorer(const SelectArgs& args, uint32_t r, uint32_t l)
+      : a(args), row(r), b(r / args.H), h(r - r / args.H * args.H), lane(l), sub(l % LPB) {}
+
+  __device__ __forceinline__ void load_bounds(uint32_t i, u32x4a& lo, u32x4a& hi) const {
     uint32_t blk = (uint32_t)a.pg.table[(size_t)b * a.pg.max_blocks + i];
     if (blk >= a.pg.n_blocks) blk = 0;
     const uint16_t* p = a.bounds + (((uint64_t)blk * a.H + h) * 2) * D + 8 * sub;
-    lo[r] = *(const u32x4a*)p;
-    hi[r] = *(const u32x4a*)(p + D);
+    lo = *(const u32x4a*)p;
+    hi = *(const u32x4a*)(p + D);
   }
-  uint32_t best[ROUNDS] = {};
-  for (uint32_t g0 = 0; g0 < a.G; g0 += 4) {
-    double q[4][8];
+
+  // query heads g0 .. g0 + 3 (past the last: that one)
+  __device__ __forceinline__ void load_heads(uint32_t g0) {
 #pragma unroll
     for (uint32_t g = 0; g < 4; ++g) {
       const uint64_t at = ((uint64_t)row * a.G + min(g0 + g, a.G - 1)) * D + 8 * sub;
@@ -235,58 +223,99 @@ __global__ __launch_bounds__(kBlockThreads) void block_score_kernel(SelectArgs a
 #pragma unroll
       for (int k = 0; k < 8; ++k) q[g][k] = (double)__builtin_fmaf(x[k], 0.0f, x[k]);
     }
-#pragma unroll
-    for (uint32_t r = 0; r < ROUNDS; ++r) {
-      double acc[4] = {};
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const uint32_t wl = lo[r][k / 2], wh = hi[r][k / 2];
-        const double x = (double)__uint_as_float(k % 2 ? wl & 0xFFFF0000u : wl << 16);
-        const double y = (double)__uint_as_float(k % 2 ? wh & 0xFFFF0000u : wh << 16);
-        const double mid = x + y, wide = y - x;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          acc[g] = __builtin_fma(q[g][k], mid, acc[g]);
-          acc[g] = __builtin_fma(__builtin_fabs(q[g][k]), wide, acc[g]);
-        }
-      }
-      // lanes with bit 0 of sub clear keep heads 0 and 1, then bit 1 picks one of the two
-      const bool b0 = (lane & 1) != 0, b1 = (lane & 2) != 0;
-      const double k0 = b0 ? acc[2] : acc[0], s0 = b0 ? acc[0] : acc[2];
-      const double k1 = b0 ? acc[3] : acc[1], s1 = b0 ? acc[1] : acc[3];
-      const double t0 = k0 + lane_xor_f64<1>(s0), t1 = k1 + lane_xor_f64<1>(s1);
-      double s = (b1 ? t1 : t0) + lane_xor_f64<2>(b1 ? t0 : t1);
-      s += lane_xor_f64<4>(s);
-      if constexpr (LPB == 16) s += lane_xor_f64<8>(s);
-      // the heads' scores lie on the lanes of a quad
-      uint32_t key = score_key((float)(0.5 * s));
-      key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0xB1, 0xF, 0xF, true));
-      key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0x4E, 0xF, 0xF, true));
-      best[r] = max(best[r], key);
-    }
   }
+
+  // the largest of the four heads' scores, as key
+  __device__ __forceinline__ uint32_t score(const u32x4a& lo, const u32x4a& hi) const {
+    double acc[4] = {};
 #pragma unroll
-  for (uint32_t r = 0; r < ROUNDS; ++r)
-    if (sub == 0 && i0 + r * BPW < n) a.keys[(uint64_t)row * a.n_keys + i0 + r * BPW] = best[r];
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t wl = lo[k / 2], wh = hi[k / 2];
+      const double x = (double)__uint_as_float(k % 2 ? wl & 0xFFFF0000u : wl << 16);
+      const double y = (double)__uint_as_float(k % 2 ? wh & 0xFFFF0000u : wh << 16);
+      const double mid = x + y, wide = y - x;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        acc[g] = __builtin_fma(q[g][k], mid, acc[g]);
+        acc[g] = __builtin_fma(__builtin_fabs(q[g][k]), wide, acc[g]);
+      }
+    }
+    // lanes with bit 0 of sub clear keep heads 0 and 1, then bit 1 picks one of the two
+    const bool b0 = (lane & 1) != 0, b1 = (lane & 2) != 0;
+    const double k0 = b0 ? acc[2] : acc[0], s0 = b0 ? acc[0] : acc[2];
+    const double k1 = b0 ? acc[3] : acc[1], s1 = b0 ? acc[1] : acc[3];
+    const double t0 = k0 + lane_xor_f64<1>(s0), t1 = k1 + lane_xor_f64<1>(s1);
+    double s = (b1 ? t1 : t0) + lane_xor_f64<2>(b1 ? t0 : t1);
+    s += lane_xor_f64<4>(s);
+    if constexpr (LPB == 16) s += lane_xor_f64<8>(s);
+    // the heads' scores lie on the lanes of a quad
+    uint32_t key = score_key((float)(0.5 * s));
+    key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0xB1, 0xF, 0xF, true));
+    return max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0x4E, 0xF, 0xF, true));
+  }
+};
+
+// Scores of the blocks of one (sequence, KV head) of up to 4 query heads: `rounds` times 4 or 8 blocks a
+// wave, the next ones requested before the present ones are worked on.  Bound by the bounds' bytes:
+// 64 sequences of 2,032 blocks, d = 128, 533 MB in 110 us (4.8 TB/s); a few blocks by the start, 3.6 us.
+template <int D, bool F32>
+__global__ __launch_bounds__(kBlockThreads) void block_score_kernel(SelectArgs a, uint32_t rounds) {
+  constexpr uint32_t LPB = D / 8, BPW = kWave / LPB, STEP = BPW * kWavesPerBlock;
+  const uint32_t per = STEP * rounds, per_row = (a.n_keys + per - 1) / per;    // blocks, workgroups of a row
+  const uint32_t row = blockIdx.x / per_row;
+  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  Scorer<D, F32> s(a, row, lane);
+  const uint32_t first = (blockIdx.x - row * per_row) * per + wave * BPW;
+  uint32_t ctx;
+  const uint32_t n = min(context_blocks(a, s.b, ctx), (blockIdx.x - row * per_row + 1) * per);
+  if (first >= n) return;
+  uint32_t* const keys = a.keys + (uint64_t)row * a.n_keys;
+  uint32_t i = first + lane / LPB;
+  u32x4a lo, hi;
+  s.load_bounds(min(i, n - 1), lo, hi);
+  s.load_heads(0);
+  for (; i - lane / LPB < n; i += STEP) {
+    const u32x4a l = lo, u = hi;
+    s.load_bounds(min(i + STEP, n - 1), lo, hi);
+    const uint32_t key = s.score(l, u);
+    if (s.sub == 0 && i < n) keys[i] = key;
+  }
 }
 
-// The n_sel largest keys of one (sequence, KV head), the lower block first among equals; the first
-// and last blocks stand outside the comparison.  The key of the last kept block is found from its
-// top down, 8 bits a step, by counting the keys of the range that is left by their next 8 bits (most
-// steps end early: as soon as all of a bin are kept).  A wave looks after KPT x 64 consecutive keys
-// (KPT = 0: of any number, read again in every step), 64 at a time in ascending order, so that places
-// among the kept come from counted ballots.  Bound by the vector instructions of its one workgroup,
-// six passes over the keys.
-template <int THREADS, int KPT>
-__global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
-  constexpr uint32_t WAVES = THREADS / kWave;
-  __shared__ __attribute__((aligned(16))) uint32_t s_hist[256];
-  __shared__ uint32_t s_wave[2][WAVES], s_pick[3];
-  const uint32_t row = blockIdx.x, b = row / a.H, t = threadIdx.x;
-  const uint32_t lane = t % kWave, wave = t / kWave;
+// The same of more query heads: two rounds of blocks a wave, which stay in registers while the heads
+// pass by.  (By the loop above, a pass over the blocks for every 4 heads: 16,375 blocks of 8 heads 16 us
+// in place of 12.8.)
+template <int D, bool F32>
+__global__ __launch_bounds__(kBlockThreads) void block_score_heads_kernel(SelectArgs a) {
+  constexpr uint32_t LPB = D / 8, BPW = kWave / LPB;
+  constexpr uint32_t PER = BPW * kHeadRounds * kWavesPerBlock;
+  const uint32_t per_row = (a.n_keys + PER - 1) / PER;
+  const uint32_t row = blockIdx.x / per_row;
+  const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  Scorer<D, F32> s(a, row, lane);
+  const uint32_t i0 = (blockIdx.x - row * per_row) * PER + wave * BPW * kHeadRounds + lane / LPB;
   uint32_t ctx;
-  const uint32_t n = context_blocks(a, b, ctx);
-  const uint32_t keep = min(n, a.n_sel);
+  const uint32_t n = context_blocks(a, s.b, ctx);
+  if (i0 - lane / LPB >= n) return;
+  u32x4a lo[kHeadRounds], hi[kHeadRounds];
+#pragma unroll
+  for (uint32_t r = 0; r < kHeadRounds; ++r) s.load_bounds(min(i0 + r * BPW, n - 1), lo[r], hi[r]);
+  uint32_t best[kHeadRounds] = {};
+  for (uint32_t g0 = 0; g0 < a.G; g0 += 4) {
+    s.load_heads(g0);
+#pragma unroll
+    for (uint32_t r = 0; r < kHeadRounds; ++r) best[r] = max(best[r], s.score(lo[r], hi[r]));
+  }
+#pragma unroll
+  for (uint32_t r = 0; r < kHeadRounds; ++r)
+    if (s.sub == 0 && i0 + r * BPW < n) a.keys[(uint64_t)row * a.n_keys + i0 + r * BPW] = best[r];
+}
+
+// What a list holds without a comparison: its length, the first and last blocks.  False where that is
+// all of it.
+template <int THREADS>
+__device__ __forceinline__ bool begin_list(const SelectArgs& a, uint32_t row, uint32_t n, uint32_t ctx) {
+  const uint32_t t = threadIdx.x, keep = min(n, a.n_sel);
   int32_t* const out = a.blocks + (uint64_t)row * a.n_sel;
   // the last block of the context is always kept, and it alone may be short
   if (t == 0)
@@ -294,14 +323,31 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
                                          ((n - 1) << a.pg.block_log2));
   if (n <= a.n_sel) {
     for (uint32_t i = t; i < a.n_sel; i += THREADS) out[i] = i < n ? (int32_t)i : -1;
-    return;
+    return false;
   }
+  const uint32_t ends = a.n_first + a.n_last;
+  for (uint32_t i = t; i < ends; i += THREADS)
+    out[i < a.n_first ? i : a.n_sel - ends + i] = (int32_t)(i < a.n_first ? i : n - ends + i);
+  return a.n_sel > ends;
+}
+
+// The rest of the list: the largest of the keys of the blocks between the ends (keys: from n_first
+// on), the lower block first among equals.  The key of the last kept block is found from its
+// top down, 8 bits a step, by counting the keys of the range that is left by their next 8 bits (most
+// steps end early: as soon as all of a bin are kept).  A wave looks after KPT x 64 consecutive keys
+// (KPT = 0: of any number, read again in every step), 64 at a time in ascending order, so that places
+// among the kept come from counted ballots.  Bound by the vector instructions of its one workgroup,
+// six passes over the keys.
+template <int THREADS, int KPT>
+__device__ __forceinline__ void choose(const SelectArgs& a, uint32_t row, uint32_t n,
+                                       const uint32_t* keys) {
+  constexpr uint32_t WAVES = THREADS / kWave;
+  __shared__ __attribute__((aligned(16))) uint32_t s_hist[256];
+  __shared__ uint32_t s_wave[2][WAVES], s_pick[3];
+  const uint32_t t = threadIdx.x, lane = t % kWave, wave = t / kWave;
+  int32_t* const out = a.blocks + (uint64_t)row * a.n_sel;
   const uint32_t want = a.n_sel - a.n_first - a.n_last;              // kept between the ends
   const uint32_t m = n - a.n_first - a.n_last;                       // blocks between them
-  for (uint32_t i = t; i < a.n_first + a.n_last; i += THREADS)
-    out[i < a.n_first ? i : want + i] = (int32_t)(i < a.n_first ? i : m + i);
-  if (want == 0) return;
-  const uint32_t* const keys = a.keys + (uint64_t)row * a.n_keys + a.n_first;
   const uint32_t per = KPT > 0 ? (uint32_t)KPT : (m + THREADS - 1) / THREADS;
   const uint32_t first = wave * per * kWave + lane;
   uint32_t k[KPT > 0 ? KPT : 1];
@@ -391,6 +437,43 @@ __global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
   });
 }
 
+template <int THREADS, int KPT>
+__global__ __launch_bounds__(THREADS) void block_select_kernel(SelectArgs a) {
+  const uint32_t row = blockIdx.x;
+  uint32_t ctx;
+  const uint32_t n = context_blocks(a, row / a.H, ctx);
+  if (begin_list<THREADS>(a, row, n, ctx))
+    choose<THREADS, KPT>(a, row, n, a.keys + (uint64_t)row * a.n_keys + a.n_first);
+}
+
+// Scores and choice of a short list in one workgroup, the keys in LDS: a launch less.
+constexpr uint32_t kShortThreads = 512;
+
+template <int D, bool F32>
+__global__ __launch_bounds__(kShortThreads) void block_short_kernel(SelectArgs a) {
+  constexpr uint32_t LPB = D / 8, BPW = kWave / LPB, STEP = BPW * kShortThreads / kWave;
+  __shared__ uint32_t s_keys[kShortThreads];
+  const uint32_t row = blockIdx.x, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  Scorer<D, F32> s(a, row, lane);
+  uint32_t ctx;
+  const uint32_t n = context_blocks(a, s.b, ctx);
+  if (!begin_list<kShortThreads>(a, row, n, ctx)) return;
+  for (uint32_t g0 = 0; g0 < a.G; g0 += 4) {
+    uint32_t i = wave * BPW + lane / LPB;
+    u32x4a lo, hi;
+    s.load_bounds(min(i, n - 1), lo, hi);
+    s.load_heads(g0);
+    for (; i - lane / LPB < n; i += STEP) {
+      const u32x4a l = lo, u = hi;
+      s.load_bounds(min(i + STEP, n - 1), lo, hi);
+      const uint32_t key = s.score(l, u);
+      if (s.sub == 0 && i < n) s_keys[i] = g0 == 0 ? key : max(key, s_keys[i]);
+    }
+  }
+  __syncthreads();
+  choose<kShortThreads, 1>(a, row, n, s_keys + a.n_first);
+}
+
 // Tokens of a block up to which a group takes it.  32 layers, 16 sequences, 8 heads of d = 128, us by
 // a group and by a wave: 1 token 4.8 and 6.4, 8 tokens 5.2 and 11.5, 16 tokens 7.2 and 11.2; 4,099
 // tokens of one sequence 58 and 53, of which the copy rate of the device (5.15 TB/s) would need 54.
@@ -410,10 +493,35 @@ void launch_bounds(const KeyBoundsArgs& a, hipStream_t s) {
                        dim3(kBlockThreads), 0, s, a);
 }
 
+// Rounds of a wave: the device full with 4 workgroups a compute unit, 16 at most.  us a call, 4 / 8
+// workgroups: 513 blocks of 16 sequences 13.6 / 14.7, 2,032 blocks 31.7 / 29.3, of 64 sequences 120 / 119.
+constexpr uint32_t kScorePlaces = 4, kScoreRounds = 16;
+
 template <int D, bool F32>
 void launch_scores(const SelectArgs& a, hipStream_t s) {
-  const uint32_t per_row = (a.n_keys + kScoreBlocks<D> - 1) / kScoreBlocks<D>;
-  hipLaunchKernelGGL((block_score_kernel<D, F32>), dim3(per_row * a.B * a.H), dim3(kBlockThreads), 0, s, a);
+  constexpr uint32_t STEP = kBlockThreads / (D / 8);
+  if (a.G > 4) {
+    const uint32_t per_row = (a.n_keys + STEP * kHeadRounds - 1) / (STEP * kHeadRounds);
+    hipLaunchKernelGGL((block_score_heads_kernel<D, F32>), dim3(per_row * a.B * a.H), dim3(kBlockThreads), 0, s, a);
+    return;
+  }
+  const uint64_t steps = (uint64_t)a.B * a.H * ((a.n_keys + STEP - 1) / STEP);
+  const uint32_t rounds = (uint32_t)min(max(steps / (kScorePlaces * a.cus), (uint64_t)1), (uint64_t)kScoreRounds);
+  const uint32_t per_row = (a.n_keys + STEP * rounds - 1) / (STEP * rounds);
+  hipLaunchKernelGGL((block_score_kernel<D, F32>), dim3(per_row * a.B * a.H), dim3(kBlockThreads), 0, s, a,
+                     rounds);
+}
+
+// Lists up to which one workgroup scores and chooses; the second, where there are as many lists as
+// compute units.  us on the device, by one launch and by two: one sequence (8 lists) of 129 blocks 7.4
+// and 7.1 (a call of the host 9 and 13), of 250 blocks 9.6 and 7.1; 64 sequences of 129 blocks 10.7 and
+// 14.7, of 511 blocks 24 and 41.
+constexpr uint32_t kShortKeys = 160, kManyShortKeys = 512;
+
+template <int D, bool F32>
+void launch_short(const SelectArgs& a, hipStream_t s) {
+  static_assert(kManyShortKeys <= kShortThreads, "a key a thread");
+  hipLaunchKernelGGL((block_short_kernel<D, F32>), dim3(a.B * a.H), dim3(kShortThreads), 0, s, a);
 }
 
 // The keys of a list stay in registers where 1024 threads can hold them, of the fewest that do: a list
@@ -444,9 +552,13 @@ int tvq_launch_key_bounds(const tvq::KeyBoundsArgs& a, int d, bool f32, void* st
 
 int tvq_launch_select(const tvq::SelectArgs& a, int d, bool f32, void* stream) {
   hipStream_t s = (hipStream_t)stream;
-  if (d == 128) f32 ? tvq::launch_scores<128, true>(a, s) : tvq::launch_scores<128, false>(a, s);
-  else if (d == 64) f32 ? tvq::launch_scores<64, true>(a, s) : tvq::launch_scores<64, false>(a, s);
+  const bool apart = a.n_keys > (a.B * a.H >= a.cus ? tvq::kManyShortKeys : tvq::kShortKeys);
+  if (d == 128 && apart) f32 ? tvq::launch_scores<128, true>(a, s) : tvq::launch_scores<128, false>(a, s);
+  else if (d == 64 && apart) f32 ? tvq::launch_scores<64, true>(a, s) : tvq::launch_scores<64, false>(a, s);
+  else if (d == 128) f32 ? tvq::launch_short<128, true>(a, s) : tvq::launch_short<128, false>(a, s);
+  else if (d == 64) f32 ? tvq::launch_short<64, true>(a, s) : tvq::launch_short<64, false>(a, s);
   else return -1;
+  if (!apart) return hipGetLastError() == hipSuccess ? 0 : -2;
   if (hipGetLastError() != hipSuccess) return -2;
   tvq::launch_select(a, s);
   return hipGetLastError() == hipSuccess ? 0 : -2;

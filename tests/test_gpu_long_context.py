@@ -428,6 +428,9 @@ SELECT = [
     (64, 1, 1, 32, 6000, 192000, [192000, 33000], 1100, 0, 1),
     (64, 1, 2, 32, 17003, 544096, [544096, 530000, 7000, 50000], 201, 0, 1),
     (64, 1, 1, 32, 16600, 531200, [531200], 1300, 5, 9),
+    # as many lists as compute units; several rounds of blocks a wave
+    (64, 8, 2, 32, 201, 6432, [6432 - 190 * i for i in range(33)], 7, 1, 2),
+    (128, 4, 1, 32, 601, 19232, [19232 - 900 * i for i in range(20)], 33, 0, 1),
 ]
 
 
